@@ -4,43 +4,20 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <mutex>
-#include <string>
 
 #include "pd.h"
+#include "pd_host.h"
 #include "pd_kernels.h"
 
 namespace {
 
-thread_local std::string g_last_error;
-
-pd_status fail(pd_status s, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof(buf), fmt, ap);
-  va_end(ap);
-  g_last_error = buf;
-  return s;
-}
-
-pd_status ok() {
-  g_last_error.clear();
-  return PD_OK;
-}
+using namespace pd_host;
 
 constexpr int kMaxChunks = 1024;
 constexpr int kMaxChunkLen = 4096;
 constexpr int kMaxSplits = 64;
 constexpr int kMaxCompactRows = 1 << 20;   // prefix rows of a compact decode call
-constexpr size_t kAlign = 256;
-
-size_t round_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int cdiv(long long a, long long b) { return (int)((a + b - 1) / b); }
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 pd_status check_dims(const pd_dims* d) {
   if (!d) return fail(PD_ERR_NULL_PTR, "dims is NULL");
@@ -228,31 +205,6 @@ size_t decode_ws_bytes(const pd_dims* d, int S) {
   return round_up(rows * d->head_dim * sizeof(float)) + round_up(rows * sizeof(float));
 }
 
-pd_status check_ws(void* ws, size_t have, size_t need) {
-  if (need == 0) return PD_OK;
-  if (!ws) return fail(PD_ERR_WORKSPACE, "workspace is NULL but %zu bytes are needed", need);
-  if (!aligned16(ws)) return fail(PD_ERR_MISALIGNED, "workspace is not 16-byte aligned");
-  if (have < need) return fail(PD_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
-  return PD_OK;
-}
-
-#define PD_REQUIRE_PTR(p)                                               \
-  do {                                                                  \
-    if (!(p)) return fail(PD_ERR_NULL_PTR, "pointer '%s' is NULL", #p); \
-    if (!aligned16(p)) return fail(PD_ERR_MISALIGNED, "pointer '%s' is not 16-byte aligned", #p); \
-  } while (0)
-
-#define PD_RETURN_IF(st)          \
-  do {                            \
-    pd_status _s = (st);          \
-    if (_s != PD_OK) return _s;   \
-  } while (0)
-
-pd_status hip_status(hipError_t e, const char* what) {
-  if (e == hipSuccess) return ok();
-  return fail(PD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
 }  // namespace
 
 extern "C" {
@@ -280,7 +232,7 @@ const char* pd_status_string(pd_status s) {
   return "PD_ERR_UNKNOWN";
 }
 
-const char* pd_last_error_message(void) { return g_last_error.c_str(); }
+const char* pd_last_error_message(void) { return pd_host::last_error().c_str(); }
 
 size_t pd_cache_bytes(const pd_dims* d) {
   if (check_dims(d) != PD_OK) return 0;
