@@ -58,7 +58,8 @@ typedef enum {
   PD_ERR_HIP = 6          /* a kernel launch failed                               */
 } pd_status;
 
-typedef enum { PD_BF16 = 0, PD_FP32 = 1 } pd_dtype;
+/* PD_FP8_E4M3: the elements of a paged cache only (see pd_paged_dims). */
+typedef enum { PD_BF16 = 0, PD_FP32 = 1, PD_FP8_E4M3 = 2 } pd_dtype;
 
 typedef struct {
   int32_t batch;        /* B >= 1                                                   */
@@ -302,6 +303,152 @@ pd_status pd_gather_joint(const pd_dims *dims, int32_t top_k, int32_t tok_budget
                           const void *q_qm, const void *k_qm, const void *v_qm, double rope_base,
                           void *q_joint, void *k_joint, void *v_joint, void *k_pref, void *v_pref,
                           void *stream);
+
+/*
+ * Head norms and rotary positions: what turns the projected query and key rows
+ * of n_rows tokens into the rows that the attention entry points take.  For
+ * every head row x (d elements) of q and k
+ *   y_i = x_i * w_i / sqrt(mean_j x_j^2 + eps)        (w_q for q, w_k for k)
+ * and then, for i = 0..d/2-1 with the angle a = pos[t] * rope_base^(-2i/d),
+ *   out_i = y_i cos a - y_{i+d/2} sin a,  out_{i+d/2} = y_{i+d/2} cos a + y_i sin a.
+ * w_q (w_k) NULL: the query (key) heads are not normalised.  rope_base = 0: no
+ * rotation, pos may be NULL.  Norms in fp32; the angle in double precision,
+ * reduced to one turn before its sine and cosine are taken in fp32; one
+ * rounding to the element type at the end.
+ *
+ * Inputs (element type dtype, PD_BF16 or PD_FP32): q, k: row t of q holds its
+ *   n_heads_q heads of d = head_dim contiguous elements one after another at
+ *   element t * q_stride (likewise k, n_heads_kv, k_stride), so that both may
+ *   point into the rows of a fused projection.  w_q, w_k [d].  pos int32
+ *   [n_rows], any values.
+ * Outputs: q_out, k_out, laid out the same with q_out_stride, k_out_stride.
+ *   q_out may be q itself with the same stride (k_out likewise); other overlaps
+ *   of inputs and outputs, and of q_out and k_out, are not allowed.
+ * Sizes: n_rows >= 0 (0: nothing is done), n_heads_q >= 0 and n_heads_kv >= 0
+ *   with at least one head in all (the pointers of a tensor without heads may
+ *   be NULL), d in {64, 128}, strides >= heads * d and multiples of 16 bytes,
+ *   eps >= 0 finite, rope_base >= 0 finite.  No workspace.
+ */
+pd_status pd_qk_norm_rope(int32_t n_rows, int32_t n_heads_q, int32_t n_heads_kv, int32_t head_dim, int32_t dtype,
+                          const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                          const void *w_q, const void *w_k, float eps, const int32_t *pos, double rope_base,
+                          void *q_out, int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *stream);
+
+/*
+ * Paged key/value cache: sequences of different and growing lengths over one
+ * pool of pages.  A page holds R = page_rows consecutive rows of one sequence,
+ * for every KV head.  Position p of sequence b is row p % R of page
+ * page_table[b][p / R].
+ *
+ * With cache_dtype = PD_FP8_E4M3 a head's row is held as E4M3 values (the OCP
+ * format with NaN and no infinities, largest value 448) times a power of two:
+ * e is the least exponent with max|x| <= 448 * 2^e over the row's finite
+ * elements, within -100..120 (-100 for a row of zeros), the values are
+ * x * 2^-e rounded to nearest even, and the byte e + 127 is kept beside them.
+ * NaN and infinities become NaN.  Scaling by a power of two is exact, so that
+ * the rounding to E4M3 is the only one.
+ */
+typedef struct {
+  int32_t batch;        /* B, 1..65536 sequences                                    */
+  int32_t new_len;      /* L_n >= 1: places for the new rows of a sequence           */
+  int32_t n_heads_q;    /* H_q >= 1                                                  */
+  int32_t n_heads_kv;   /* H_kv >= 1, divides H_q                                    */
+  int32_t head_dim;     /* d, 64 or 128                                              */
+  int32_t dtype;        /* of queries, new rows and outputs: PD_BF16 or PD_FP32      */
+  int32_t cache_dtype;  /* of the pages: dtype, or PD_FP8_E4M3 when dtype = PD_BF16  */
+  int32_t page_rows;    /* R: 16, 32, 64, 128 or 256                                 */
+  int32_t n_pages;      /* pages in the pool, >= 1                                   */
+  int32_t max_pages;    /* entries of a sequence in page_table, >= 1                 */
+  float sm_scale;       /* softmax scale; <= 0 selects 1/sqrt(d)                     */
+  int32_t causal;       /* 1: a new row sees the positions up to its own; 0: all
+                           kv_len positions                                          */
+} pd_paged_dims;
+
+/* Device memory of the cache.  kv_len and new_rows are read on the device:
+ * values outside 0..max_pages*R and 0..L_n are taken as the nearer bound. */
+typedef struct {
+  void *k_pages, *v_pages;    /* [n_pages][H_kv][R][d], cache_dtype                  */
+  uint8_t *k_exp, *v_exp;     /* [n_pages][H_kv][R] exponent bytes; PD_FP8_E4M3 only,
+                                 else NULL                                           */
+  void *k_bounds;             /* [n_pages][H_kv][2][d], dtype: per channel the least
+                                 and the largest key of a page, as given to
+                                 pd_paged_append (before quantisation); NULL: not
+                                 kept (pd_paged_select needs it)                     */
+  const int32_t *page_table;  /* [B][max_pages]; only entries of pages that hold rows
+                                 are read                                            */
+  const int32_t *kv_len;      /* [B] rows of each sequence, the new ones included    */
+  const int32_t *new_rows;    /* [B] new rows of each sequence, or NULL: L_n each    */
+} pd_paged_cache;
+
+/*
+ * Writes new rows into the pages: row r < new_rows[b] of sequence b is its
+ * position kv_len[b] - new_rows[b] + r (positions below 0 are not written).
+ * k_new, v_new (dtype): row (b, r) holds its H_kv heads of d contiguous
+ * elements at element (b * L_n + r) * stride.  k_bounds, where kept: a page
+ * whose row 0 is written begins with the new rows of this call, any other page's
+ * bounds are widened by them; NaNs do not count.  Everything else in the pool is left as it
+ * is.  A page may be written through one sequence only in a call.  A page id
+ * outside 0..n_pages-1 is not written to.
+ * Strides: >= H_kv * d, multiples of 16 bytes.  No workspace.
+ */
+pd_status pd_paged_append(const pd_paged_dims *dims, const pd_paged_cache *cache, const void *k_new,
+                          int64_t k_stride, const void *v_new, int64_t v_stride, void *stream);
+
+/*
+ * Reads rows back: k_out, v_out [B][H_kv][n_rows][d] (dtype) receive positions
+ * first..first+n_rows-1 of every sequence, dequantised; this is the prefix
+ * layout of pd_sparse_decode_attn_compact.  Rows of positions >= kv_len[b] are
+ * left as they were.  A page id outside 0..n_pages-1 gives NaN rows.  What an
+ * E4M3 value times its power of two stands for is exact in bf16, except that
+ * 2^128, which magnitudes from 1.9375 * 2^127 round to, reads as infinity.
+ * Sizes: first >= 0, n_rows >= 1, first + n_rows <= max_pages * R.  No workspace.
+ */
+pd_status pd_paged_read(const pd_paged_dims *dims, const pd_paged_cache *cache, int32_t first, int32_t n_rows,
+                        void *k_out, void *v_out, void *stream);
+
+/*
+ * Chooses pages for each query: for sequence b and KV head g, a page's score is
+ * the largest, over the G * new_rows[b] query rows of the group (G = H_q/H_kv),
+ * of  sum_i q_i * (q_i >= 0 ? hi_i : lo_i)  with the page's bounds lo, hi: no
+ * key of the page has a larger product with the row.  Products and sums are in
+ * double precision.  The top_k best of the sequence's ceil(kv_len/R) pages are
+ * kept; its first n_first and last n_last pages rank above all others, a NaN score above every
+ * number, and ties go to the lower page.
+ * q [B][L_n][H_q][d] (dtype).  page_idx int32 [B][H_kv][top_k]: the kept pages'
+ * indices in the sequence (p / R), ascending; -1 behind the last where the
+ * sequence has fewer pages.
+ * Sizes: 1 <= top_k <= max_pages <= 65536, n_first, n_last >= 0.
+ * workspace: >= pd_paged_workspace_bytes(dims, top_k, 0) bytes.
+ */
+pd_status pd_paged_select(const pd_paged_dims *dims, const pd_paged_cache *cache, const void *q, int32_t top_k,
+                          int32_t n_first, int32_t n_last, int32_t *page_idx, void *workspace, size_t ws_bytes,
+                          void *stream);
+
+/*
+ * Attention of the new rows over the pages: row r < new_rows[b] of sequence b
+ * attends to the positions p of its cache with p <= kv_len[b] - new_rows[b] + r
+ * (causal = 1) or p < kv_len[b] (causal = 0), its own rows included (append
+ * first).  page_idx NULL (top_k = 0): all pages; otherwise [B][H_kv][top_k]
+ * page indices as written by pd_paged_select: KV head g attends to the visible
+ * positions of those pages alone (an entry outside 0..max_pages-1 is skipped, a
+ * page named twice counts twice).
+ * q, o [B][L_n][H_q][d] (dtype); lse fp32 [B][H_q][L_n] natural-log row LSE, or
+ * NULL.  Rows r >= new_rows[b] of o and lse are left as they were.  A row that
+ * sees no position, or only scores of -inf, gets o = 0 and lse = -inf.  What
+ * the pages hold behind kv_len is never used, whatever its bits.  A page id
+ * outside 0..n_pages-1 that is needed makes the group's rows NaN.
+ * The lengths are known on the device alone: the split of long sequences over
+ * workgroups, and their join, are planned there.
+ * workspace: >= pd_paged_workspace_bytes(dims, top_k, 1) bytes (may be 0, then
+ * workspace may be NULL).
+ */
+pd_status pd_paged_attn(const pd_paged_dims *dims, const pd_paged_cache *cache, const void *q,
+                        const int32_t *page_idx, int32_t top_k, void *o, float *lse, void *workspace,
+                        size_t ws_bytes, void *stream);
+
+/* Workspace bytes for `which` = 0 pd_paged_select, 1 pd_paged_attn (top_k = 0:
+ * over all pages).  Returns 0 for invalid arguments. */
+size_t pd_paged_workspace_bytes(const pd_paged_dims *dims, int32_t top_k, int32_t which);
 
 /* Bytes of ONE of k_cache / v_cache for one layer: B*N*H_kv*(1+C)*d*elem. */
 size_t pd_cache_bytes(const pd_dims *dims);

@@ -25,6 +25,8 @@ that each step can be checked against the paper by eye:
   attention-space reading of Eqs. 3-4), and selection of the K lowest.
 * ``full_mask`` -- full-mask cache construction: the kept rows and the query
   rows rotated to continuous positions and encoded jointly.
+* ``paged`` -- head norms with rotary positions, the 8-bit rows of a paged cache,
+  page choice and attention of new rows over the pages.
 
 Parity status of each function is stated in its docstring ("pinned by ...").
 """
@@ -48,8 +50,10 @@ from .static import (
 )
 from .chunk_score import prefill_chunk_score_ref, select_ranked_ref
 from .full_mask import rope_rotate_ref, joint_deltas, joint_rows_ref, joint_attention_ref
+from . import paged
 
 __all__ = [
+    "paged",
     "chunk_rows",
     "chunk_probs",
     "prefill_unit_ref",

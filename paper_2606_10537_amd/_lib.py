@@ -13,7 +13,7 @@ from dataclasses import dataclass
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libpd.so")
 
-PD_BF16, PD_FP32 = 0, 1
+PD_BF16, PD_FP32, PD_FP8_E4M3 = 0, 1, 2
 STATUS = {0: "PD_OK", 1: "PD_ERR_NULL_PTR", 2: "PD_ERR_BAD_DIMS", 3: "PD_ERR_UNSUPPORTED",
           4: "PD_ERR_MISALIGNED", 5: "PD_ERR_WORKSPACE", 6: "PD_ERR_HIP"}
 
@@ -21,7 +21,8 @@ EXPORTS = ["pd_prefill_chunks", "pd_score_select", "pd_sparse_decode_attn", "pd_
            "pd_workspace_bytes", "pd_decode_splits", "pd_status_string", "pd_last_error_message",
            "pd_version", "pd_mfma_rate_probe", "pd_score_select_static", "pd_gather_selected",
            "pd_sparse_decode_attn_compact", "pd_compact_workspace_bytes", "pd_select_ranked",
-           "pd_gather_joint", "pd_score_select_noalloc"]
+           "pd_gather_joint", "pd_score_select_noalloc", "pd_qk_norm_rope", "pd_paged_append", "pd_paged_read",
+           "pd_paged_select", "pd_paged_attn", "pd_paged_workspace_bytes"]
 
 
 class PdError(RuntimeError):
@@ -67,6 +68,21 @@ class Dims:
         return PdDims(self.batch, self.n_chunks, self.chunk_len, self.q_len, self.m_len, self.dec_len,
                       self.n_heads_q, self.n_heads_kv, self.head_dim, self.dtype, self.sm_scale,
                       self.qm_per_chunk, self.out_fp32, self.tok_score_dir)
+
+
+class PagedDims(ctypes.Structure):
+    """Sizes of a paged cache and of the calls on it (see pd_paged_dims in include/pd.h); built with keywords."""
+    _fields_ = [
+        ("batch", ctypes.c_int32), ("new_len", ctypes.c_int32), ("n_heads_q", ctypes.c_int32),
+        ("n_heads_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("cache_dtype", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("causal", ctypes.c_int32),
+    ]
+
+
+class PdPagedCache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k_pages", "v_pages", "k_exp", "v_exp", "k_bounds", "page_table",
+                                               "kv_len", "new_rows")]
 
 
 _lib = None
@@ -118,6 +134,20 @@ def load(path: str = LIB_PATH):
     lib.pd_compact_workspace_bytes.restype = sz
     lib.pd_mfma_rate_probe.argtypes = [i32, i32, vp, vp]
     lib.pd_mfma_rate_probe.restype = ctypes.c_int
+    pp, cp, i64 = ctypes.POINTER(PagedDims), ctypes.POINTER(PdPagedCache), ctypes.c_int64
+    lib.pd_qk_norm_rope.argtypes = [i32] * 5 + [vp, i64, vp, i64, vp, vp, ctypes.c_float, vp, ctypes.c_double,
+                                                vp, i64, vp, i64, vp]
+    lib.pd_qk_norm_rope.restype = ctypes.c_int
+    lib.pd_paged_append.argtypes = [pp, cp, vp, i64, vp, i64, vp]
+    lib.pd_paged_append.restype = ctypes.c_int
+    lib.pd_paged_read.argtypes = [pp, cp, i32, i32, vp, vp, vp]
+    lib.pd_paged_read.restype = ctypes.c_int
+    lib.pd_paged_select.argtypes = [pp, cp, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.pd_paged_select.restype = ctypes.c_int
+    lib.pd_paged_attn.argtypes = [pp, cp, vp, vp, i32, vp, vp, vp, sz, vp]
+    lib.pd_paged_attn.restype = ctypes.c_int
+    lib.pd_paged_workspace_bytes.argtypes = [pp, i32, i32]
+    lib.pd_paged_workspace_bytes.restype = sz
     lib.pd_version.argtypes = []
     lib.pd_version.restype = ctypes.c_char_p
     _lib = lib
@@ -250,3 +280,179 @@ def pd_compact_workspace_bytes(dims: Dims, n_sel, num_splits=0) -> int:
 def pd_mfma_rate_probe(n_workgroups, iters, sink, stream=None):
     """Launch the MFMA-rate diagnostic (n_workgroups * 4 * iters * 8 * 32768 FLOP)."""
     _check(load().pd_mfma_rate_probe(n_workgroups, iters, _ptr(sink), _stream(stream)))
+
+
+# --------------------------------------------------------------------------- paged cache
+# Sequences of these calls grow and shrink between calls, so the tensors' types, sizes and
+# device are checked here against the sizes that the kernels will index by.
+
+def _types(dtype):
+    import torch
+    return {PD_BF16: (torch.bfloat16,), PD_FP32: (torch.float32,),
+            PD_FP8_E4M3: (torch.float8_e4m3fn, torch.uint8)}.get(dtype, ())
+
+
+def _same_device(device):
+    import torch
+    if device != torch.cuda.current_device():
+        raise ValueError(f"tensors on cuda:{device} while cuda:{torch.cuda.current_device()} is current")
+
+
+def _checked(name, t, shape, types, device=None):
+    """Device pointer of a contiguous tensor of this shape and one of these types; on `device`, or the current one."""
+    if t.dtype not in types:
+        raise ValueError(f"{name} has type {t.dtype}, wanted {' or '.join(map(str, types))}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if device is None:
+        _same_device(t.get_device())
+    elif t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, the cache on cuda:{device}")
+    return t.data_ptr()
+
+
+def _rows(name, t, shape, types, device=None):
+    """Pointer and row stride of a tensor [..., heads, d] whose heads lie one after another in a row and whose rows
+    (all dimensions before the heads) lie one stride apart."""
+    if t.dtype not in types:
+        raise ValueError(f"{name} has type {t.dtype}, wanted {' or '.join(map(str, types))}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
+    heads, d = shape[-2], shape[-1]
+    strides = t.stride()
+    if (d > 1 and strides[-1] != 1) or (heads > 1 and strides[-2] != d):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    lead = [(n, s) for n, s in zip(shape[:-2], strides[:-2]) if n != 1]
+    stride = lead[-1][1] if lead else heads * d
+    want = stride
+    for n, s in reversed(lead):
+        if s != want:
+            raise ValueError(f"{name}: its rows must lie one stride apart")
+        want = n * s
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on the GPU")
+    if device is None:
+        _same_device(t.get_device())
+    elif t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, not on cuda:{device}")
+    return t.data_ptr(), stride
+
+
+def _space(workspace, device):
+    """Pointer and size of a workspace, or of none."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device:
+        raise ValueError(f"the workspace is on cuda:{workspace.get_device()}, the cache on cuda:{device}")
+    return _ptr(workspace), _nbytes(workspace)
+
+
+class PagedCache:
+    """The tensors of a paged cache (see pd_paged_cache in include/pd.h), checked against `dims` once and kept alive.
+
+    k_pages, v_pages [n_pages][H_kv][R][d]; page_table int32 [B][max_pages]; kv_len, new_rows int32 [B]; k_exp, v_exp
+    uint8 [n_pages][H_kv][R] for PD_FP8_E4M3; k_bounds [n_pages][H_kv][2][d]."""
+
+    def __init__(self, dims, k_pages, v_pages, page_table, kv_len, new_rows=None, k_exp=None, v_exp=None,
+                 k_bounds=None):
+        import torch
+        d = dims
+        pool = (d.n_pages, d.n_heads_kv, d.page_rows)
+        if not k_pages.is_cuda:
+            raise ValueError("k_pages must be on the GPU")
+        self.device = k_pages.get_device()
+        self.dims = PagedDims.from_buffer_copy(d)
+        self.tensors = (k_pages, v_pages, k_exp, v_exp, k_bounds, page_table, kv_len, new_rows)
+        if (d.cache_dtype == PD_FP8_E4M3) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
+            raise ValueError("k_exp and v_exp belong to a cache of PD_FP8_E4M3, and only to it")
+        shapes = {"k_pages": (pool + (d.head_dim,), _types(d.cache_dtype)),
+                  "v_pages": (pool + (d.head_dim,), _types(d.cache_dtype)),
+                  "k_exp": (pool, (torch.uint8,)), "v_exp": (pool, (torch.uint8,)),
+                  "k_bounds": (pool[:2] + (2, d.head_dim), _types(d.dtype)),
+                  "page_table": ((d.batch, d.max_pages), (torch.int32,)),
+                  "kv_len": ((d.batch,), (torch.int32,)), "new_rows": ((d.batch,), (torch.int32,))}
+        self.c = PdPagedCache()
+        for (name, _), t in zip(PdPagedCache._fields_, self.tensors):
+            if t is not None:
+                setattr(self.c, name, _checked(name, t, *shapes[name], self.device))
+
+    def _for(self, dims):
+        """The descriptor, for a call with these sizes: those of the pool and the batch are the cache's own."""
+        own = self.dims
+        if dims is not own and any(getattr(dims, f) != getattr(own, f) for f in (
+                "batch", "n_heads_kv", "head_dim", "dtype", "cache_dtype", "page_rows", "n_pages", "max_pages")):
+            raise ValueError("dims differ from those that the cache was made with")
+        _same_device(self.device)
+        return ctypes.byref(self.c)
+
+
+def pd_qk_norm_rope(q, k, w_q, w_k, eps, pos, rope_base, q_out, k_out, stream=None):
+    """Head norms and rotary positions of q [T, H_q, d] and k [T, H_kv, d] (see include/pd.h); rows may be strided;
+    k and k_out None: queries alone; w_q, w_k None: no norm; rope_base 0: no rotation."""
+    import torch
+    kinds = {torch.bfloat16: PD_BF16, torch.float32: PD_FP32}
+    if q.dtype not in kinds or q.dim() != 3:
+        raise ValueError(f"q must be [rows, heads, d] in bf16 or fp32, got {tuple(q.shape)} {q.dtype}")
+    (T, hq, d), types, device = q.shape, (q.dtype,), q.get_device()
+    qp, qs = _rows("q", q, q.shape, types)
+    qo, qos = _rows("q_out", q_out, q.shape, types, device)
+    hkv, kp, ks, ko, kos = 0, None, 0, None, 0
+    if k is not None:
+        hkv = k.shape[1] if k.dim() == 3 else 0
+        kp, ks = _rows("k", k, (T, hkv, d), types, device)
+        ko, kos = _rows("k_out", k_out, (T, hkv, d), types, device)
+    wq = None if w_q is None else _checked("w_q", w_q, (d,), types, device)
+    wk = None if w_k is None else _checked("w_k", w_k, (d,), types, device)
+    pp = None if pos is None else _checked("pos", pos, (T,), (torch.int32,), device)
+    _check(load().pd_qk_norm_rope(T, hq, hkv, d, kinds[q.dtype], qp, qs, kp, ks, wq, wk, eps, pp, float(rope_base),
+                                  qo, qos, ko, kos, _stream(stream)))
+
+
+def pd_paged_workspace_bytes(dims: PagedDims, top_k=0, which=1) -> int:
+    return load().pd_paged_workspace_bytes(ctypes.byref(dims), top_k, which)
+
+
+def pd_paged_append(dims: PagedDims, cache: PagedCache, k_new, v_new, stream=None):
+    """New rows k_new, v_new [B, L_n, H_kv, d] into the pages (see include/pd.h); rows may be strided."""
+    shape, c = (dims.batch, dims.new_len, dims.n_heads_kv, dims.head_dim), cache._for(dims)
+    kp, ks = _rows("k_new", k_new, shape, _types(dims.dtype), cache.device)
+    vp, vs = _rows("v_new", v_new, shape, _types(dims.dtype), cache.device)
+    _check(load().pd_paged_append(ctypes.byref(dims), c, kp, ks, vp, vs, _stream(stream)))
+
+
+def pd_paged_read(dims: PagedDims, cache: PagedCache, first, n_rows, k_out, v_out, stream=None):
+    """Positions first..first+n_rows-1 of every sequence into k_out, v_out [B, H_kv, n_rows, d] (see include/pd.h)."""
+    shape, c = (dims.batch, dims.n_heads_kv, n_rows, dims.head_dim), cache._for(dims)
+    _check(load().pd_paged_read(ctypes.byref(dims), c, first, n_rows,
+                                _checked("k_out", k_out, shape, _types(dims.dtype), cache.device),
+                                _checked("v_out", v_out, shape, _types(dims.dtype), cache.device), _stream(stream)))
+
+
+def pd_paged_select(dims: PagedDims, cache: PagedCache, q, top_k, n_first, n_last, page_idx, workspace, stream=None):
+    """The top_k pages of each (sequence, KV head) by a bound on their scores (see include/pd.h)."""
+    import torch
+    c, dev = cache._for(dims), cache.device
+    _check(load().pd_paged_select(
+        ctypes.byref(dims), c, _checked("q", q, (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim),
+                                        _types(dims.dtype), dev), top_k, n_first, n_last,
+        _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), (torch.int32,), dev),
+        *_space(workspace, dev), _stream(stream)))
+
+
+def pd_paged_attn(dims: PagedDims, cache: PagedCache, q, o, lse=None, page_idx=None, workspace=None, stream=None):
+    """Attention of the new rows q [B, L_n, H_q, d] over the pages, or over those of page_idx [B, H_kv, K] (see
+    include/pd.h); lse [B, H_q, L_n] fp32 or None."""
+    import torch
+    c, dev = cache._for(dims), cache.device
+    shape = (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim)
+    top_k = 0 if page_idx is None else page_idx.shape[-1]
+    _check(load().pd_paged_attn(
+        ctypes.byref(dims), c, _checked("q", q, shape, _types(dims.dtype), dev),
+        None if page_idx is None else _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), (torch.int32,), dev),
+        top_k, _checked("o", o, shape, _types(dims.dtype), dev),
+        None if lse is None else _checked("lse", lse, (dims.batch, dims.n_heads_q, dims.new_len), (torch.float32,), dev),
+        *_space(workspace, dev), _stream(stream)))

@@ -1,0 +1,561 @@
+// The paged cache but for its attention: head norms with rotary positions, writing
+// rows into the pages (quantised to E4M3 where the cache is), reading them back,
+// and the choice of pages by a bound on their scores.
+#include "paged_common.h"
+
+namespace pd {
+
+// ---------------------------------------------------------------------------
+// Head norms and rotary positions.
+//
+// y = x * w / sqrt(mean x^2 + eps), then (y_i, y_{i+d/2}) turned by pos * base^(-2i/d).
+// Every element is read and written once; nothing else is moved, so memory bounds
+// it.  A lane holds 16 bytes of a head, d/E lanes a head row, so a wave takes 64 E / d
+// heads at a time: the sum of squares is a butterfly over those lanes, and the
+// partner of a rotation sits d/2E lanes away.
+//
+// The angle is taken in turns in double precision (pos * f_i, f_i = base^(-2i/d) /
+// 2 pi), reduced by its nearest integer, and only then rounded to fp32: its error
+// stays below 1e-7 turns up to positions of 2^31, and costs one double product for
+// each pair and wave, not one for each head.  Lanes 0..d/2-1 take a pair each and
+// hand the sines and cosines over through LDS.
+//
+// U: head groups a wave loads before it uses the first.
+template <bool BF16, int D, int U>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int groups) {
+  constexpr int E = BF16 ? 8 : 4;       // elements of a lane
+  constexpr int L = D / E;              // lanes of a head
+  constexpr int HP = 64 / L;            // heads of a wave
+  __shared__ float2 table[4][D / 2];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % L;
+  const long long item = (long long)block_id() * 4 + wave;
+  const long long row = item / groups;
+  if (row >= a.rows) return;
+  const int h0 = (int)(item - row * groups) * HP * U + lane / L, H = a.Hq + a.Hkv;
+  const char* src[U];
+  char* dst[U];
+  Row16<BF16> x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int h = h0 + u * HP;
+    const int t = h >= a.Hq ? 1 : 0;
+    const long long el = (long long)(t ? h - a.Hq : h) * D + c * E;
+    src[u] = (const char*)(t ? a.x[1] : a.x[0]) + (row * (t ? a.xs[1] : a.xs[0]) + el) * (BF16 ? 2 : 4);
+    dst[u] = (char*)(t ? a.y[1] : a.y[0]) + (row * (t ? a.ys[1] : a.ys[0]) + el) * (BF16 ? 2 : 4);
+    if (h < H) x[u].load(src[u]);
+    else x[u].zero();
+  }
+  float cs[E], sn[E];
+  if (a.pos) {
+    // The wave's own part of the table: written and read by one wave, in order.
+    if (lane < D / 2) {
+      const double f = exp2(-(double)lane * a.log2_step) * 0.15915494309189535;
+      const double turn = (double)a.pos[row] * f;
+      float s, co;
+      sincospif(2.0f * (float)(turn - rint(turn)), &s, &co);
+      table[wave][lane] = make_float2(co, s);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float2 z = table[wave][(c % (L / 2)) * E + e];
+      cs[e] = z.x;
+      sn[e] = c < L / 2 ? -z.y : z.y;   // out_i = y_i cos - y' sin, out_{i+d/2} = y_{i+d/2} cos + y' sin
+    }
+  }
+  Row16<BF16> wv[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    if (a.w[t]) wv[t].load((const char*)a.w[t] + c * 16);
+    else wv[t].zero();
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int h = h0 + u * HP, t = h >= a.Hq ? 1 : 0;
+    float y[E];
+    x[u].unpack(y);
+    if (a.w[0] || a.w[1]) {
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s = fmaf(y[e], y[e], s);
+#pragma unroll
+      for (int m = 1; m < L; m *= 2) s += __shfl_xor(s, m);
+      const float r = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
+      float w[E], w1[E];
+      wv[0].unpack(w);
+      wv[1].unpack(w1);
+      const bool norm = t ? a.w[1] != nullptr : a.w[0] != nullptr;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float z = y[e] * r * (t ? w1[e] : w[e]);
+        y[e] = norm ? z : y[e];
+      }
+    }
+    if (a.pos) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float p = __shfl_xor(y[e], L / 2);
+        y[e] = fmaf(p, sn[e], y[e] * cs[e]);
+      }
+    }
+    x[u].pack(y);
+    if (h < H) x[u].store(dst[u]);
+  }
+}
+
+template <bool BF16, int D>
+hipError_t norm_rope_of(const NormRopeArgs& a, hipStream_t s) {
+  constexpr int HP = 64 / (D / (BF16 ? 8 : 4));
+  const int H = a.Hq + a.Hkv;
+  // Four head groups a wave keep enough loads in flight where the rows fill the CUs;
+  // below that every group is a wave of its own.
+  const bool wide = a.rows * ((H + 4 * HP - 1) / (4 * HP)) >= 8 * 256;
+  const int per = wide ? 4 * HP : HP, groups = (H + per - 1) / per;
+  const dim3 grid = grid_xy((a.rows * groups + 3) / 4);
+  if (wide) hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, 4>), grid, dim3(256), 0, s, a, groups);
+  else hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, 1>), grid, dim3(256), 0, s, a, groups);
+  return hipGetLastError();
+}
+
+hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s) {
+  if (a.bf16) return a.D == 128 ? norm_rope_of<true, 128>(a, s) : norm_rope_of<true, 64>(a, s);
+  return a.D == 128 ? norm_rope_of<false, 128>(a, s) : norm_rope_of<false, 64>(a, s);
+}
+
+// ---------------------------------------------------------------------------
+// Writing rows into the pages.
+//
+// One workgroup per (sequence, page that new rows fall into, KV head): the bounds of a
+// page need all its rows, and so no atomics are needed.  A lane holds 16 bytes
+// of a row as in the norm kernel; waves 0 and 2 take the key rows, 1 and 3 the
+// value rows.  Memory bounds it: every new row is read once and written once.
+//
+// Quantisation: e from the bits of the largest magnitude (448 = 1.75 * 2^8, so e is the
+// binary exponent minus 8, or one more where the mantissa exceeds 1.75), the
+// product with 2^-e is exact, and the conversion rounds to nearest even.
+template <bool BF16, bool FP8, int D>
+__global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, HP = 64 / L, EB = BF16 ? 2 : 4;
+  __shared__ float bound[2][2][D];
+  const PagedArgs& p = a.c;
+  const long long id = block_id();
+  const int h = (int)(id % p.Hkv);
+  const long long bj = id / p.Hkv;
+  const int b = (int)(bj / a.pages);
+  if (b >= p.B) return;
+  const int len = paged_len(p, b), n_new = paged_new(p, b);
+  const int start = len - n_new;                       // position of new row 0; below 0: rows that are not written
+  const int j = (max(start, 0) >> p.log2R) + (int)(bj % a.pages);
+  const int lo = max(max(start, 0), j << p.log2R), hi = min(len, (j + 1) << p.log2R);
+  if (lo >= hi) return;
+  const int page = p.page_table[(long long)b * p.max_pages + j];
+  if ((unsigned)page >= (unsigned)p.n_pages) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % L;
+  const int kv = wave & 1;
+  const char* src = (const char*)(kv ? a.v_new : a.k_new) + ((long long)h * D + c * E) * EB;
+  const long long stride = (kv ? a.vs : a.ks) * EB;
+  const long long base = ((long long)page * p.Hkv + h) * p.R;   // row of the pool
+  char* dst = (char*)(kv ? p.v_pages : p.k_pages) + (base * D + c * E) * (FP8 ? 1 : EB);
+  uint8_t* ex = FP8 ? (kv ? p.v_exp : p.k_exp) + base : nullptr;
+  const bool bounds = p.k_bounds && kv == 0;
+  float least[E], most[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    least[e] = INFINITY;
+    most[e] = -INFINITY;
+  }
+  constexpr int U = 4;   // rows of a lane in flight
+  for (int r0 = lo + (wave >> 1) * HP * U; r0 < hi; r0 += 2 * HP * U) {
+    Row16<BF16> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = min(r0 + u * HP + lane / L, hi - 1);
+      x[u].load(src + ((long long)b * p.Ln + (r - start)) * stride);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * HP + lane / L;
+      const bool live = r < hi;
+      const int slot = r & (p.R - 1);
+      float y[E];
+      x[u].unpack(y);
+      if (bounds && live) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          least[e] = fminf(least[e], y[e]);
+          most[e] = fmaxf(most[e], y[e]);
+        }
+      }
+      if constexpr (FP8) {
+        float m = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float t = fabsf(y[e]);
+          m = fmaxf(m, t < INFINITY ? t : 0.f);
+        }
+#pragma unroll
+        for (int k = 1; k < L; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+        const uint32_t bits = __float_as_uint(m);
+        const int e2 = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
+        const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float z[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[e] = y[4 * k + e] * inv;
+            z[e] = fabsf(y[4 * k + e]) < INFINITY ? z[e] : NAN;
+          }
+          int v = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+          w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], v, true);
+        }
+        if (live) {
+          *(u32x2*)(dst + (long long)slot * D) = u32x2{w[0], w[1]};
+          if (c == 0) ex[slot] = (uint8_t)(e2 + 127);
+        }
+      } else {
+        if (live) x[u].store(dst + (long long)slot * D * EB);
+      }
+    }
+  }
+  if (!p.k_bounds) return;
+  if (bounds) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+#pragma unroll
+      for (int k = L; k < 64; k *= 2) {
+        least[e] = fminf(least[e], __shfl_xor(least[e], k));
+        most[e] = fmaxf(most[e], __shfl_xor(most[e], k));
+      }
+      if (lane < L) {
+        bound[wave >> 1][0][c * E + e] = least[e];
+        bound[wave >> 1][1][c * E + e] = most[e];
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * D; i += 256) {
+    const bool up = i >= D;
+    const int ch = up ? i - D : i;
+    float x = bound[0][up][ch];
+    x = up ? fmaxf(x, bound[1][up][ch]) : fminf(x, bound[1][up][ch]);
+    const long long at = ((long long)page * p.Hkv + h) * 2 * D + i;
+    if constexpr (BF16) {
+      uint16_t* q = (uint16_t*)p.k_bounds + at;
+      if ((lo & (p.R - 1)) != 0) x = up ? fmaxf(x, bf16_to_f32(*q)) : fminf(x, bf16_to_f32(*q));
+      *q = f32_to_bf16(x);
+    } else {
+      float* q = (float*)p.k_bounds + at;
+      if ((lo & (p.R - 1)) != 0) x = up ? fmaxf(x, *q) : fminf(x, *q);
+      *q = x;
+    }
+  }
+}
+
+hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
+  const dim3 grid = grid_xy((long long)a.c.B * a.pages * a.c.Hkv);
+#define PD_APPEND(BF, F8)                                                                                \
+  do {                                                                                                   \
+    if (a.c.D == 128) hipLaunchKernelGGL((paged_append_kernel<BF, F8, 128>), grid, dim3(256), 0, s, a);  \
+    else hipLaunchKernelGGL((paged_append_kernel<BF, F8, 64>), grid, dim3(256), 0, s, a);                \
+  } while (0)
+  if (a.c.fp8) PD_APPEND(true, true);
+  else if (a.c.bf16) PD_APPEND(true, false);
+  else PD_APPEND(false, false);
+#undef PD_APPEND
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Reading rows back: a lane writes 16 bytes of the output, a wave consecutive
+// rows of one (sequence, head), which lie beside each other in the pages too.
+// Memory bounds it.
+template <bool BF16, bool FP8, int D>
+__global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int blocks) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, RP = 256 / L, EB = BF16 ? 2 : 4, U = 4;
+  const PagedArgs& p = a.c;
+  const long long id = block_id();
+  const long long bh = id / blocks;
+  const int b = (int)(bh / p.Hkv), h = (int)(bh % p.Hkv);
+  if (b >= p.B) return;
+  const int len = paged_len(p, b), c = threadIdx.x % L;
+  const int row0 = (int)(id % blocks) * RP * U + threadIdx.x / L;
+  const int end = min(len - a.first, a.n);
+  if ((int)(id % blocks) * RP * U >= end) return;
+  const int32_t* table = p.page_table + (long long)b * p.max_pages;
+  long long at[U];
+  bool bad[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int pos = a.first + min(row0 + u * RP, end - 1);
+    int page = table[pos >> p.log2R];
+    bad[u] = (unsigned)page >= (unsigned)p.n_pages;
+    if (bad[u]) page = 0;
+    at[u] = ((long long)page * p.Hkv + h) * p.R + (pos & (p.R - 1));
+  }
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    const char* src = (const char*)(kv ? p.v_pages : p.k_pages);
+    char* out = (char*)(kv ? a.v_out : a.k_out) + (bh * a.n * D + c * E) * EB;
+    if constexpr (FP8) {
+      const uint8_t* ex = kv ? p.v_exp : p.k_exp;
+      u32x2 w[U];
+      float s[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        w[u] = *(const u32x2*)(src + at[u] * D + c * E);
+        s[u] = exp_to_scale(ex[at[u]]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[u][k], false);
+          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[u][k], true);
+          y[4 * k] = lo[0] * s[u];
+          y[4 * k + 1] = lo[1] * s[u];
+          y[4 * k + 2] = hi[0] * s[u];
+          y[4 * k + 3] = hi[1] * s[u];
+        }
+        Row16<true> x;
+        x.pack(y);
+        if (bad[u]) x.nan();
+        if (row0 + u * RP < end) x.store(out + (long long)(row0 + u * RP) * D * EB);
+      }
+    } else {
+      Row16<BF16> x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u].load(src + (at[u] * D + c * E) * EB);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (bad[u]) x[u].nan();
+        if (row0 + u * RP < end) x[u].store(out + (long long)(row0 + u * RP) * D * EB);
+      }
+    }
+  }
+}
+
+template <bool BF16, bool FP8, int D>
+hipError_t read_of(const ReadArgs& a, hipStream_t s) {
+  constexpr int rows = 256 / (D / (BF16 ? 8 : 4)) * 4;
+  const int blocks = (a.n + rows - 1) / rows;
+  hipLaunchKernelGGL((paged_read_kernel<BF16, FP8, D>), grid_xy((long long)a.c.B * a.c.Hkv * blocks), dim3(256), 0,
+                     s, a, blocks);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s) {
+  const bool wide = a.c.D == 128;
+  if (a.c.fp8) return wide ? read_of<true, true, 128>(a, s) : read_of<true, true, 64>(a, s);
+  if (a.c.bf16) return wide ? read_of<true, false, 128>(a, s) : read_of<true, false, 64>(a, s);
+  return wide ? read_of<false, false, 128>(a, s) : read_of<false, false, 64>(a, s);
+}
+
+// ---------------------------------------------------------------------------
+// Page scores: max over the group's query rows of sum_i q_i * (q_i >= 0 ? hi_i : lo_i).
+//
+// Pages whose scores differ in the last bits of an fp32 sum have to come out in the
+// same order whatever the order of summation, so products and sums are double: the
+// product of two bf16 is exact there, and a sum of d of them too unless their
+// exponents lie more than 30 apart.  The bounds are read once per block of query rows
+// and converted once; memory bounds it for few query rows (16 lanes or more read a
+// page's bounds in whole lines), the double FMAs (one per element and row) for many.
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a, int blocks) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = 256 / L, EB = BF16 ? 2 : 4, QR = 16;
+  __shared__ __align__(16) float q[QR][D];
+  const PagedArgs& p = a.c;
+  const long long id = block_id();
+  const long long bh = id / blocks;
+  const int b = (int)(bh / p.Hkv), g = (int)(bh % p.Hkv);
+  if (b >= p.B) return;
+  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
+  const int rows = paged_new(p, b) * p.G;
+  const int j0 = (int)(id % blocks) * PP, c = threadIdx.x % L;
+  if (j0 >= pages) return;
+  const int j = j0 + threadIdx.x / L;
+  int page = p.page_table[(long long)b * p.max_pages + min(j, pages - 1)];
+  const bool bad = (unsigned)page >= (unsigned)p.n_pages;
+  if (bad) page = 0;
+  const char* src = (const char*)p.k_bounds + (((long long)page * p.Hkv + g) * 2 * D + c * E) * EB;
+  Row16<BF16> lo, hi;
+  lo.load(src);
+  hi.load(src + D * EB);
+  float l32[E], h32[E];
+  lo.unpack(l32);
+  hi.unpack(h32);
+  double best = -INFINITY;
+  bool nan = bad;
+  for (int r0 = 0; r0 < rows; r0 += QR) {
+    const int n = min(QR, rows - r0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < n * L; i += 256) {
+      const int r = r0 + i / L, ch = i % L;
+      Row16<BF16> x;
+      x.load((const char*)a.q +
+             ((((long long)b * p.Ln + r / p.G) * p.Hq + (long long)g * p.G + r % p.G) * D + ch * E) * EB);
+      x.unpack(&q[i / L][ch * E]);
+    }
+    __syncthreads();
+    for (int r = 0; r < n; ++r) {
+      double s = 0.0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float x = q[r][c * E + e];
+        s = fma((double)x, (double)(x >= 0.f ? h32[e] : l32[e]), s);
+      }
+#pragma unroll
+      for (int m = 1; m < L; m *= 2) s += __shfl_xor(s, m);
+      nan = nan || s != s;
+      best = fmax(best, s);
+    }
+  }
+  if (c == 0 && j < pages) a.score[bh * p.max_pages + j] = nan ? (double)NAN : best;
+}
+
+// The top_k pages of one (sequence, KV head), ascending.  Scores map to 64-bit keys whose
+// order is theirs; a radix descent of eight bits a pass finds the key of the last page
+// kept, then the pages above it and the lowest ones equal to it are written in order.
+// The latency of those passes bounds it: a thread keeps its keys in registers for up
+// to KPT pages and reads them again from the workspace beyond.
+constexpr int kSelectThreads = 512;
+
+__device__ __forceinline__ uint64_t page_key(const PageSelectArgs& a, const double* score, int j, int pages) {
+  if (j < a.n_first || j >= pages - a.n_last) return ~0ull;
+  const double s = score[j];
+  if (s != s) return ~0ull - 1;
+  const uint64_t u = __builtin_bit_cast(uint64_t, s == 0.0 ? 0.0 : s);
+  return (u >> 63) ? ~u : (u | (1ull << 63));
+}
+
+// Exclusive sum over the workgroup of one value per thread; total: the sum of all.
+__device__ __forceinline__ int block_prefix(int x, int* lds, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int s = x;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const int y = __shfl_up(s, m);
+    if (lane >= m) s += y;
+  }
+  __syncthreads();
+  if (lane == 63) lds[wave] = s;
+  __syncthreads();
+  int before = 0, all = 0;
+  for (int w = 0; w < kSelectThreads / 64; ++w) {
+    if (w < wave) before += lds[w];
+    all += lds[w];
+  }
+  *total = all;
+  return before + s - x;
+}
+
+template <int KPT>
+__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectArgs a) {
+  __shared__ uint32_t hist[256];
+  __shared__ int sums[kSelectThreads / 64];
+  __shared__ int pick[2];
+  const PagedArgs& p = a.c;
+  const long long bh = block_id();
+  const int b = (int)(bh / p.Hkv), tid = threadIdx.x;
+  if (b >= p.B) return;
+  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
+  const double* score = a.score + bh * p.max_pages;
+  int32_t* out = a.page_idx + bh * a.top_k;
+  const int k = min(a.top_k, pages);
+  for (int i = k + tid; i < a.top_k; i += kSelectThreads) out[i] = -1;
+  if (k == pages) {
+    for (int i = tid; i < k; i += kSelectThreads) out[i] = i;
+    return;
+  }
+  uint64_t key[KPT];
+  const int turns = (pages + kSelectThreads - 1) / kSelectThreads;
+#pragma unroll
+  for (int t = 0; t < KPT; ++t)
+    key[t] = t * kSelectThreads + tid < pages ? page_key(a, score, t * kSelectThreads + tid, pages) : 0;
+  auto key_of = [&](int t) {   // t beyond the registers: pages there are many of
+    return t * kSelectThreads + tid < pages ? page_key(a, score, t * kSelectThreads + tid, pages) : 0;
+  };
+  uint64_t prefix = 0;
+  int need = k;                // pages still to be taken among those that match the prefix
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
+    __syncthreads();
+    auto count = [&](uint64_t x, int j) {
+      if (j < pages && (shift == 56 || (x >> (shift + 8)) == (prefix >> (shift + 8))))
+        atomicAdd(&hist[(x >> shift) & 255], 1u);
+    };
+#pragma unroll
+    for (int t = 0; t < KPT; ++t) count(key[t], t * kSelectThreads + tid);
+    for (int t = KPT; t < turns; ++t) count(key_of(t), t * kSelectThreads + tid);
+    __syncthreads();
+    if (tid < 64) {
+      // Lane l owns digits 255-4l .. 252-4l, the highest first.
+      int own[4], s = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s += own[i] = (int)hist[255 - 4 * tid - i];
+      int incl = s;
+#pragma unroll
+      for (int m = 1; m < 64; m *= 2) {
+        const int y = __shfl_up(incl, m);
+        if (tid >= m) incl += y;
+      }
+      int before = incl - s;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (before < need && before + own[i] >= need) {
+          pick[0] = 255 - 4 * tid - i;
+          pick[1] = before;
+        }
+        before += own[i];
+      }
+    }
+    __syncthreads();
+    prefix |= (uint64_t)pick[0] << shift;
+    need -= pick[1];
+    __syncthreads();
+  }
+  // prefix: the key of the last page kept; need: how many pages with that key are.
+  int written = 0, equal = 0;
+  for (int t = 0; t < turns; ++t) {
+    const int j = t * kSelectThreads + tid;
+    uint64_t x = 0;
+    if (t < KPT) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i)
+        if (i == t) x = key[i];
+    } else {
+      x = key_of(t);
+    }
+    int total;
+    const int same = j < pages && x == prefix;
+    const int rank = equal + block_prefix(same, sums, &total);
+    equal += total;
+    const int keep = j < pages && (x > prefix || (same && rank < need));
+    const int at = written + block_prefix(keep, sums, &total);
+    written += total;
+    if (keep) out[at] = j;
+  }
+}
+
+hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s) {
+  const PagedArgs& p = a.c;
+  const int per = 256 / (p.D / (p.bf16 ? 8 : 4)), blocks = (p.max_pages + per - 1) / per;
+  const dim3 grid = grid_xy((long long)p.B * p.Hkv * blocks);
+  if (p.bf16) {
+    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<true, 128>), grid, dim3(256), 0, s, a, blocks);
+    else hipLaunchKernelGGL((page_score_kernel<true, 64>), grid, dim3(256), 0, s, a, blocks);
+  } else {
+    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<false, 128>), grid, dim3(256), 0, s, a, blocks);
+    else hipLaunchKernelGGL((page_score_kernel<false, 64>), grid, dim3(256), 0, s, a, blocks);
+  }
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 sg = grid_xy((long long)p.B * p.Hkv);
+  if (p.max_pages <= kSelectThreads) hipLaunchKernelGGL(page_select_kernel<1>, sg, dim3(kSelectThreads), 0, s, a);
+  else hipLaunchKernelGGL(page_select_kernel<8>, sg, dim3(kSelectThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace pd

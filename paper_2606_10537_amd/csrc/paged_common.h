@@ -1,0 +1,50 @@
+// Device helpers of the paged-cache kernels.
+#pragma once
+#include "paged_kernels.h"
+#include "pd_common.h"
+#include "pd_kernels.h"
+
+namespace pd {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// 16 bytes of a row: eight bf16 or four fp32.
+template <bool BF16>
+struct Row16 {
+  u32x4 v;
+  __device__ __forceinline__ void load(const void* p) { v = *(const u32x4*)p; }
+  __device__ __forceinline__ void store(void* p) const { *(u32x4*)p = v; }
+  __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ void nan() { v = u32x4{kNanWord, kNanWord, kNanWord, kNanWord}; }
+  __device__ __forceinline__ void unpack(float* y) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) {
+        y[2 * i] = __uint_as_float(v[i] << 16);
+        y[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+      } else {
+        y[i] = __uint_as_float(v[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ void pack(const float* y) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (BF16) v[i] = pack_bf16x2(y[2 * i], y[2 * i + 1]);
+      else v[i] = __float_as_uint(y[i]);
+    }
+  }
+};
+
+// 2^e of an exponent byte e + 127 (27..247).
+__device__ __forceinline__ float exp_to_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Rows and new rows of a sequence, within what the cache and the call have room for.
+__device__ __forceinline__ int paged_len(const PagedArgs& p, int b) {
+  return min(max(p.kv_len[b], 0), p.max_pages << p.log2R);
+}
+__device__ __forceinline__ int paged_new(const PagedArgs& p, int b) {
+  return p.new_rows ? min(max(p.new_rows[b], 0), p.Ln) : p.Ln;
+}
+
+}  // namespace pd

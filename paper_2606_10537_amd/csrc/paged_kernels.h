@@ -1,0 +1,79 @@
+// Argument blocks and launchers of the paged-cache kernels (internal to the library).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace pd {
+
+struct NormRopeArgs {
+  const void *x[2];      // query rows, key rows
+  void *y[2];
+  const void *w[2];      // norm weights or nullptr
+  long long xs[2], ys[2];  // row strides, elements
+  const int32_t* pos;    // nullptr: no rotation
+  long long rows;
+  int Hq, Hkv, D;
+  float eps;
+  double log2_step;      // log2(rope_base) * 2 / d: pair i turns by pos * 2^(-i * log2_step)
+  bool bf16;
+};
+hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s);
+
+// The cache as the kernels see it.
+struct PagedArgs {
+  void *k_pages, *v_pages;
+  uint8_t *k_exp, *v_exp;
+  void* k_bounds;
+  const int32_t *page_table, *kv_len, *new_rows;
+  int B, Ln, Hq, Hkv, G, D, R, log2R, n_pages, max_pages, causal;
+  bool bf16, fp8;        // new rows and outputs in bf16 (else fp32); pages in E4M3
+  float scale_log2;      // softmax scale * log2(e)
+};
+
+struct AppendArgs {
+  PagedArgs c;
+  const void *k_new, *v_new;
+  long long ks, vs;      // row strides, elements
+  int pages;             // pages that the new rows of one sequence can touch
+};
+hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
+
+struct ReadArgs {
+  PagedArgs c;
+  void *k_out, *v_out;
+  int first, n;
+};
+hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s);
+
+struct PageSelectArgs {
+  PagedArgs c;
+  const void* q;
+  int top_k, n_first, n_last;
+  int32_t* page_idx;
+  double* score;         // [B][H_kv][max_pages] workspace
+};
+hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s);
+
+// Rows of one query block: the query rows of a (sequence, KV head) are taken in
+// blocks of at most this many.
+constexpr int kPagedRows = 32;
+
+struct PagedAttnArgs {
+  PagedArgs c;
+  const void* q;
+  const int32_t* page_idx;  // nullptr: all pages
+  int top_k;
+  void* o;
+  float* lse;
+  float* o_part;         // [slot][part_rows][D] sums of a workgroup whose keys are a part of its rows'
+  float* ml_part;        // [slot][part_rows][2] their maximum (log2 domain) and weight sum
+  int row_blocks, part_rows;
+  int target;            // workgroups that the keys of all sequences are cut for
+  int max_chunks;        // at most so many per (sequence, KV head, row block); 1: no parts, no join
+  long long grid;
+};
+// Keys that one workgroup takes at a time.
+int paged_block_keys(bool fp32);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+
+}  // namespace pd
