@@ -284,61 +284,68 @@ def pd_mfma_rate_probe(n_workgroups, iters, sink, stream=None):
 
 # --------------------------------------------------------------------------- paged cache
 # Sequences of these calls grow and shrink between calls, so the tensors' types, sizes and
-# device are checked here against the sizes that the kernels will index by.
+# device are checked here against the sizes that the kernels will index by.  A call of one
+# token takes the GPU a few microseconds, so what fits is told first, in a few comparisons,
+# and the reason is looked for only where something does not.
 
-def _types(dtype):
+_TYPES, _KINDS = {}, {}
+
+
+def _torch():
+    """torch, and the element types by pd_dtype and back, filled in once (loading the library imports it first)."""
     import torch
-    return {PD_BF16: (torch.bfloat16,), PD_FP32: (torch.float32,),
-            PD_FP8_E4M3: (torch.float8_e4m3fn, torch.uint8)}.get(dtype, ())
+    if not _TYPES:
+        _TYPES.update({PD_BF16: torch.bfloat16, PD_FP32: torch.float32, PD_FP8_E4M3: torch.float8_e4m3fn})
+        _KINDS.update({torch.bfloat16: PD_BF16, torch.float32: PD_FP32, "int32": torch.int32, "uint8": torch.uint8})
+    return torch
 
 
-def _same_device(device):
+def _launch_stream(stream, device):
+    """The stream's handle; the current stream of `device`, which has to be the current one, where none is given."""
     import torch
     if device != torch.cuda.current_device():
         raise ValueError(f"tensors on cuda:{device} while cuda:{torch.cuda.current_device()} is current")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return _stream(stream)
 
 
-def _checked(name, t, shape, types, device=None):
-    """Device pointer of a contiguous tensor of this shape and one of these types; on `device`, or the current one."""
-    if t.dtype not in types:
-        raise ValueError(f"{name} has type {t.dtype}, wanted {' or '.join(map(str, types))}")
-    if tuple(t.shape) != tuple(shape):
+def _refuse(name, t, shape, type_, device):
+    if t.dtype is not type_:
+        raise ValueError(f"{name} has type {t.dtype}, wanted {type_}")
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     if not t.is_cuda:
         raise ValueError(f"{name} must be on the GPU")
-    if device is None:
-        _same_device(t.get_device())
-    elif t.get_device() != device:
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, the cache on cuda:{device}")
+    raise ValueError(f"{name} is on cuda:{t.get_device()}, the call's other tensors on cuda:{device}")
+
+
+def _checked(name, t, shape, type_, device):
+    """Device pointer of a contiguous tensor of this shape and type on `device`."""
+    if t.dtype is not type_ or t.shape != shape or t.get_device() != device:
+        _refuse(name, t, shape, type_, device)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _rows(name, t, shape, types, device=None):
+def _rows(name, t, shape, type_, device):
     """Pointer and row stride of a tensor [..., heads, d] whose heads lie one after another in a row and whose rows
     (all dimensions before the heads) lie one stride apart."""
-    if t.dtype not in types:
-        raise ValueError(f"{name} has type {t.dtype}, wanted {' or '.join(map(str, types))}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, wanted {tuple(shape)}")
+    if t.dtype is not type_ or t.shape != shape or t.get_device() != device:
+        _refuse(name, t, shape, type_, device)
     heads, d = shape[-2], shape[-1]
+    if t.is_contiguous():
+        return t.data_ptr(), heads * d
     strides = t.stride()
     if (d > 1 and strides[-1] != 1) or (heads > 1 and strides[-2] != d):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
     lead = [(n, s) for n, s in zip(shape[:-2], strides[:-2]) if n != 1]
-    stride = lead[-1][1] if lead else heads * d
-    want = stride
+    stride = want = lead[-1][1] if lead else heads * d
     for n, s in reversed(lead):
         if s != want:
             raise ValueError(f"{name}: its rows must lie one stride apart")
         want = n * s
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be on the GPU")
-    if device is None:
-        _same_device(t.get_device())
-    elif t.get_device() != device:
-        raise ValueError(f"{name} is on cuda:{t.get_device()}, not on cuda:{device}")
     return t.data_ptr(), stride
 
 
@@ -347,7 +354,7 @@ def _space(workspace, device):
     if workspace is None:
         return None, 0
     if workspace.get_device() != device:
-        raise ValueError(f"the workspace is on cuda:{workspace.get_device()}, the cache on cuda:{device}")
+        raise ValueError(f"the workspace is not on cuda:{device}, as the call's other tensors")
     return _ptr(workspace), _nbytes(workspace)
 
 
@@ -355,61 +362,67 @@ class PagedCache:
     """The tensors of a paged cache (see pd_paged_cache in include/pd.h), checked against `dims` once and kept alive.
 
     k_pages, v_pages [n_pages][H_kv][R][d]; page_table int32 [B][max_pages]; kv_len, new_rows int32 [B]; k_exp, v_exp
-    uint8 [n_pages][H_kv][R] for PD_FP8_E4M3; k_bounds [n_pages][H_kv][2][d]."""
+    uint8 [n_pages][H_kv][R] for PD_FP8_E4M3; k_bounds [n_pages][H_kv][2][d].  Calls may bring dims of their own that
+    differ in new_len, n_heads_q, sm_scale and causal."""
 
     def __init__(self, dims, k_pages, v_pages, page_table, kv_len, new_rows=None, k_exp=None, v_exp=None,
                  k_bounds=None):
-        import torch
+        torch = _torch()
         d = dims
-        pool = (d.n_pages, d.n_heads_kv, d.page_rows)
         if not k_pages.is_cuda:
             raise ValueError("k_pages must be on the GPU")
+        if d.dtype not in (PD_BF16, PD_FP32) or d.cache_dtype not in _TYPES:
+            raise ValueError(f"no element type {d.dtype} or cache type {d.cache_dtype}")
         self.device = k_pages.get_device()
-        self.dims = PagedDims.from_buffer_copy(d)
+        self._key = self._sizes(dims)
         self.tensors = (k_pages, v_pages, k_exp, v_exp, k_bounds, page_table, kv_len, new_rows)
         if (d.cache_dtype == PD_FP8_E4M3) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
             raise ValueError("k_exp and v_exp belong to a cache of PD_FP8_E4M3, and only to it")
-        shapes = {"k_pages": (pool + (d.head_dim,), _types(d.cache_dtype)),
-                  "v_pages": (pool + (d.head_dim,), _types(d.cache_dtype)),
-                  "k_exp": (pool, (torch.uint8,)), "v_exp": (pool, (torch.uint8,)),
-                  "k_bounds": (pool[:2] + (2, d.head_dim), _types(d.dtype)),
-                  "page_table": ((d.batch, d.max_pages), (torch.int32,)),
-                  "kv_len": ((d.batch,), (torch.int32,)), "new_rows": ((d.batch,), (torch.int32,))}
+        self.type = _TYPES[d.dtype]
+        # E4M3 pages may also come as the bytes that they are.
+        page = k_pages.dtype if d.cache_dtype == PD_FP8_E4M3 and k_pages.dtype is torch.uint8 else _TYPES[d.cache_dtype]
+        pool = (d.n_pages, d.n_heads_kv, d.page_rows)
+        wanted = ((pool + (d.head_dim,), page), (pool + (d.head_dim,), page), (pool, torch.uint8), (pool, torch.uint8),
+                  (pool[:2] + (2, d.head_dim), self.type), ((d.batch, d.max_pages), torch.int32),
+                  ((d.batch,), torch.int32), ((d.batch,), torch.int32))
         self.c = PdPagedCache()
-        for (name, _), t in zip(PdPagedCache._fields_, self.tensors):
+        for (name, _), t, (shape, type_) in zip(PdPagedCache._fields_, self.tensors, wanted):
             if t is not None:
-                setattr(self.c, name, _checked(name, t, *shapes[name], self.device))
+                setattr(self.c, name, _checked(name, t, shape, type_, self.device))
+        self._ref = ctypes.byref(self.c)
+
+    @staticmethod
+    def _sizes(dims):
+        """What of the sizes belongs to the pool and the batch: batch, and n_heads_kv .. max_pages."""
+        raw = bytes(dims)
+        return raw[:4] + raw[12:40]
 
     def _for(self, dims):
-        """The descriptor, for a call with these sizes: those of the pool and the batch are the cache's own."""
-        own = self.dims
-        if dims is not own and any(getattr(dims, f) != getattr(own, f) for f in (
-                "batch", "n_heads_kv", "head_dim", "dtype", "cache_dtype", "page_rows", "n_pages", "max_pages")):
+        if self._sizes(dims) != self._key:
             raise ValueError("dims differ from those that the cache was made with")
-        _same_device(self.device)
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 def pd_qk_norm_rope(q, k, w_q, w_k, eps, pos, rope_base, q_out, k_out, stream=None):
     """Head norms and rotary positions of q [T, H_q, d] and k [T, H_kv, d] (see include/pd.h); rows may be strided;
     k and k_out None: queries alone; w_q, w_k None: no norm; rope_base 0: no rotation."""
-    import torch
-    kinds = {torch.bfloat16: PD_BF16, torch.float32: PD_FP32}
-    if q.dtype not in kinds or q.dim() != 3:
-        raise ValueError(f"q must be [rows, heads, d] in bf16 or fp32, got {tuple(q.shape)} {q.dtype}")
-    (T, hq, d), types, device = q.shape, (q.dtype,), q.get_device()
-    qp, qs = _rows("q", q, q.shape, types)
-    qo, qos = _rows("q_out", q_out, q.shape, types, device)
+    _torch()
+    type_, shape, device = q.dtype, q.shape, q.get_device()
+    if type_ not in _KINDS or len(shape) != 3 or device < 0:
+        raise ValueError(f"q must be [rows, heads, d] in bf16 or fp32 on the GPU, got {tuple(shape)} {type_} {q.device}")
+    T, hq, d = shape
+    qp, qs = _rows("q", q, shape, type_, device)
+    qo, qos = _rows("q_out", q_out, shape, type_, device)
     hkv, kp, ks, ko, kos = 0, None, 0, None, 0
     if k is not None:
         hkv = k.shape[1] if k.dim() == 3 else 0
-        kp, ks = _rows("k", k, (T, hkv, d), types, device)
-        ko, kos = _rows("k_out", k_out, (T, hkv, d), types, device)
-    wq = None if w_q is None else _checked("w_q", w_q, (d,), types, device)
-    wk = None if w_k is None else _checked("w_k", w_k, (d,), types, device)
-    pp = None if pos is None else _checked("pos", pos, (T,), (torch.int32,), device)
-    _check(load().pd_qk_norm_rope(T, hq, hkv, d, kinds[q.dtype], qp, qs, kp, ks, wq, wk, eps, pp, float(rope_base),
-                                  qo, qos, ko, kos, _stream(stream)))
+        kp, ks = _rows("k", k, (T, hkv, d), type_, device)
+        ko, kos = _rows("k_out", k_out, (T, hkv, d), type_, device)
+    wq = None if w_q is None else _checked("w_q", w_q, (d,), type_, device)
+    wk = None if w_k is None else _checked("w_k", w_k, (d,), type_, device)
+    pp = None if pos is None else _checked("pos", pos, (T,), _KINDS["int32"], device)
+    _check(load().pd_qk_norm_rope(T, hq, hkv, d, _KINDS[type_], qp, qs, kp, ks, wq, wk, eps, pp, rope_base,
+                                  qo, qos, ko, kos, _launch_stream(stream, device)))
 
 
 def pd_paged_workspace_bytes(dims: PagedDims, top_k=0, which=1) -> int:
@@ -418,41 +431,38 @@ def pd_paged_workspace_bytes(dims: PagedDims, top_k=0, which=1) -> int:
 
 def pd_paged_append(dims: PagedDims, cache: PagedCache, k_new, v_new, stream=None):
     """New rows k_new, v_new [B, L_n, H_kv, d] into the pages (see include/pd.h); rows may be strided."""
-    shape, c = (dims.batch, dims.new_len, dims.n_heads_kv, dims.head_dim), cache._for(dims)
-    kp, ks = _rows("k_new", k_new, shape, _types(dims.dtype), cache.device)
-    vp, vs = _rows("v_new", v_new, shape, _types(dims.dtype), cache.device)
-    _check(load().pd_paged_append(ctypes.byref(dims), c, kp, ks, vp, vs, _stream(stream)))
+    shape, c, dev = (dims.batch, dims.new_len, dims.n_heads_kv, dims.head_dim), cache._for(dims), cache.device
+    kp, ks = _rows("k_new", k_new, shape, cache.type, dev)
+    vp, vs = _rows("v_new", v_new, shape, cache.type, dev)
+    _check(load().pd_paged_append(ctypes.byref(dims), c, kp, ks, vp, vs, _launch_stream(stream, dev)))
 
 
 def pd_paged_read(dims: PagedDims, cache: PagedCache, first, n_rows, k_out, v_out, stream=None):
     """Positions first..first+n_rows-1 of every sequence into k_out, v_out [B, H_kv, n_rows, d] (see include/pd.h)."""
-    shape, c = (dims.batch, dims.n_heads_kv, n_rows, dims.head_dim), cache._for(dims)
-    _check(load().pd_paged_read(ctypes.byref(dims), c, first, n_rows,
-                                _checked("k_out", k_out, shape, _types(dims.dtype), cache.device),
-                                _checked("v_out", v_out, shape, _types(dims.dtype), cache.device), _stream(stream)))
+    shape, c, dev = (dims.batch, dims.n_heads_kv, n_rows, dims.head_dim), cache._for(dims), cache.device
+    _check(load().pd_paged_read(ctypes.byref(dims), c, first, n_rows, _checked("k_out", k_out, shape, cache.type, dev),
+                                _checked("v_out", v_out, shape, cache.type, dev), _launch_stream(stream, dev)))
 
 
 def pd_paged_select(dims: PagedDims, cache: PagedCache, q, top_k, n_first, n_last, page_idx, workspace, stream=None):
     """The top_k pages of each (sequence, KV head) by a bound on their scores (see include/pd.h)."""
-    import torch
     c, dev = cache._for(dims), cache.device
-    _check(load().pd_paged_select(
-        ctypes.byref(dims), c, _checked("q", q, (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim),
-                                        _types(dims.dtype), dev), top_k, n_first, n_last,
-        _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), (torch.int32,), dev),
-        *_space(workspace, dev), _stream(stream)))
+    qp = _checked("q", q, (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim), cache.type, dev)
+    ip = _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), _KINDS["int32"], dev)
+    _check(load().pd_paged_select(ctypes.byref(dims), c, qp, top_k, n_first, n_last, ip, *_space(workspace, dev),
+                                  _launch_stream(stream, dev)))
 
 
 def pd_paged_attn(dims: PagedDims, cache: PagedCache, q, o, lse=None, page_idx=None, workspace=None, stream=None):
     """Attention of the new rows q [B, L_n, H_q, d] over the pages, or over those of page_idx [B, H_kv, K] (see
     include/pd.h); lse [B, H_q, L_n] fp32 or None."""
-    import torch
     c, dev = cache._for(dims), cache.device
-    shape = (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim)
-    top_k = 0 if page_idx is None else page_idx.shape[-1]
-    _check(load().pd_paged_attn(
-        ctypes.byref(dims), c, _checked("q", q, shape, _types(dims.dtype), dev),
-        None if page_idx is None else _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), (torch.int32,), dev),
-        top_k, _checked("o", o, shape, _types(dims.dtype), dev),
-        None if lse is None else _checked("lse", lse, (dims.batch, dims.n_heads_q, dims.new_len), (torch.float32,), dev),
-        *_space(workspace, dev), _stream(stream)))
+    B, L, hq = dims.batch, dims.new_len, dims.n_heads_q
+    shape, top_k, ip = (B, L, hq, dims.head_dim), 0, None
+    if page_idx is not None:
+        top_k = page_idx.shape[-1]
+        ip = _checked("page_idx", page_idx, (B, dims.n_heads_kv, top_k), _KINDS["int32"], dev)
+    lp = None if lse is None else _checked("lse", lse, (B, hq, L), _TYPES[PD_FP32], dev)
+    _check(load().pd_paged_attn(ctypes.byref(dims), c, _checked("q", q, shape, cache.type, dev), ip, top_k,
+                                _checked("o", o, shape, cache.type, dev), lp, *_space(workspace, dev),
+                                _launch_stream(stream, dev)))

@@ -110,13 +110,10 @@ long long touched_pages(const pd_paged_dims* d) {
 }
 
 // --- attention: how the keys are cut, and the workspace of the parts -----------
-// Workgroups that all keys are cut for: two on every CU.
-constexpr int kTarget = 2 * pd::kNumCu;
-
 struct AttnPlan {
   int row_blocks, part_rows, max_chunks;
   long long grid;
-  size_t o_bytes, total;
+  size_t o_bytes, ml_bytes, total;
 };
 pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   const long long rows = (long long)(d->n_heads_q / d->n_heads_kv) * d->new_len;
@@ -128,12 +125,14 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   if (units >= kMaxGrid / 2 || (double)units * (double)blocks >= 9e18)
     return fail(PD_ERR_BAD_DIMS, "attention of batch=%d with new_len=%d is too large for one launch", d->batch,
                 d->new_len);
-  // A batch whose units fill the CUs anyway, or whose keys are one block each, is not cut.
-  p->max_chunks = (int)std::min<long long>(blocks, kTarget);
-  p->grid = p->max_chunks == 1 ? units : std::min(units + kTarget, units * p->max_chunks);
+  p->max_chunks = (int)std::min<long long>(blocks, pd::kPagedParts);
+  // The kernels cut with a quota of at least all blocks / kPagedParts: at most so many
+  // whole quotas, and one part that is not whole for each unit.
+  p->grid = p->max_chunks == 1 ? units : std::min(units + pd::kPagedParts, units * p->max_chunks);
   const size_t slots = p->max_chunks == 1 ? 0 : (size_t)p->grid * p->part_rows;
   p->o_bytes = round_up(slots * d->head_dim * sizeof(float));
-  p->total = p->o_bytes + round_up(slots * 2 * sizeof(float));
+  p->ml_bytes = round_up(slots * 2 * sizeof(float));
+  p->total = p->o_bytes + p->ml_bytes + (slots ? round_up((size_t)units * 4 * sizeof(int32_t)) : 0);
   return PD_OK;
 }
 
@@ -301,9 +300,9 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.lse = lse;
   a.o_part = (float*)workspace;
   a.ml_part = (float*)((char*)workspace + plan.o_bytes);
+  a.unit = (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes);
   a.row_blocks = plan.row_blocks;
   a.part_rows = plan.part_rows;
-  a.target = kTarget;
   a.max_chunks = plan.max_chunks;
   a.grid = plan.grid;
   return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");

@@ -34,74 +34,101 @@ int paged_block_keys(bool fp32) { return kPagedWaves * (fp32 ? 16 : 32); }
 // Query rows and keys of one workgroup.
 struct PagedPart {
   int b, g, rb;          // sequence, KV head, row block
-  int first, last;       // its blocks of keys
-  int parts;             // how many the row block's keys are cut into
+  int len, n_new;        // the sequence's rows and new rows
+  int first, last;       // blocks of keys of this part
+  int parts, index;      // how many the row block's keys are cut into, and which this is
   bool any;
 };
 
-// The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
-// units (KV head x row block).  With Q blocks a part, Q = ceil(all blocks / target), unit parts
-// are ceil(n_b / Q) of nearly one size, numbered by sequence, head, part, row block: at
-// most target + units parts in all.  Every wave finds its part with two sweeps over the
-// lengths, 64 sequences at a time; `find` is a part number, or, for the join, a unit
-// number (by_unit), whose first part comes back in first_part.
-__device__ __forceinline__ int paged_blocks(const PagedAttnArgs& a, int b, int block_keys) {
-  const PagedArgs& p = a.c;
-  const int len = paged_len(p, b);
-  if (len == 0 || paged_new(p, b) == 0) return 0;
-  return ((a.page_idx ? a.top_k << p.log2R : len) + block_keys - 1) / block_keys;
-}
-
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x += __shfl_xor(x, m);
+// Sum (inclusive) and maximum over the lanes up to each, on the vector units: 16 lanes at a
+// time, then the last lane of each row handed on.
+template <class F>
+__device__ __forceinline__ int wave_scan(int x, int none, F op) {
+#define PD_SCAN(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(none, x, ctrl, rows, 0xf, false))
+  PD_SCAN(0x111, 0xf);   // row_shr:1
+  PD_SCAN(0x112, 0xf);
+  PD_SCAN(0x114, 0xf);
+  PD_SCAN(0x118, 0xf);
+  PD_SCAN(0x142, 0xa);   // row_bcast:15
+  PD_SCAN(0x143, 0xc);   // row_bcast:31
+#undef PD_SCAN
   return x;
 }
 
+// The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
+// units (KV head x row block).  With a quota of Q blocks a part, a unit has ceil(n_b / Q)
+// parts of nearly one size; they are numbered by sequence, head, part, row block.  Every
+// wave finds its own part from the lengths, 64 sequences at a time.
+//
+// The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
+// card at once are cut into as few parts as give every CU one.  Otherwise parts of 16 blocks
+// or more, 2048 of them where the keys suffice, so that the workgroups of short
+// sequences and the ends of long ones fill in.  Measured, 2 CU-filling parts against 8: 8 x 32
+// heads x 8K keys 170 against 179 us, 8 x 8 heads x 32K 175 against 188, 64 ragged
+// sequences in 8 bits 474 against 382 us.
+struct PagedSeq {
+  int len, n_new, blocks;
+};
 template <int BK>
-__device__ __forceinline__ int paged_quota(const PagedAttnArgs& a, int lane) {
-  if (a.max_chunks == 1) return 1 << 30;
-  const int units = a.c.Hkv * a.row_blocks;
-  long long all = 0;
-  for (int b0 = 0; b0 < a.c.B; b0 += 64) all += wave_sum(b0 + lane < a.c.B ? paged_blocks(a, b0 + lane, BK) : 0);
-  return (int)((all * units + a.target - 1) / a.target);
+__device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int b) {
+  const PagedArgs& p = a.c;
+  PagedSeq s{0, 0, 0};
+  if (b < p.B) {
+    s.len = paged_len(p, b);
+    s.n_new = paged_new(p, b);
+    if (s.len > 0 && s.n_new > 0) s.blocks = ((a.page_idx ? a.top_k << p.log2R : s.len) + BK - 1) / BK;
+  }
+  return s;
 }
 
-__device__ __forceinline__ int parts_of(int blocks, int quota) {
-  return max(1, quota <= 1 ? blocks : (blocks + quota - 1) / quota);
-}
+__device__ __forceinline__ int parts_of(int blocks, int quota) { return blocks <= quota ? 1 : (blocks + quota - 1) / quota; }
 
 template <int BK>
 __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find, int lane) {
-  const int units = a.c.Hkv * a.row_blocks, quota = paged_quota<BK>(a, lane);
+  const PagedArgs& p = a.c;
+  const int units = p.Hkv * a.row_blocks;
+  auto add = [](int x, int y) { return x + y; };
+  auto larger = [](int x, int y) { return max(x, y); };
+  const PagedSeq head = paged_seq<BK>(a, lane);
+  int quota = 1 << 30;
+  if (a.max_chunks > 1) {
+    long long all = 0;
+    int most = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64) {
+      const int n = b0 == 0 ? head.blocks : paged_seq<BK>(a, b0 + lane).blocks;
+      all += __builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
+      most = max(most, __builtin_amdgcn_readlane(wave_scan(n, 0, larger), 63));
+    }
+    const long long seqs = (long long)p.B * units;
+    all *= units;
+    const bool even = 4 * most * seqs <= 5 * all && seqs <= 2 * kNumCu;
+    const int fill = (int)((all + kNumCu - 1) / kNumCu), fine = (int)((all + kPagedParts - 1) / kPagedParts);
+    quota = max(1, even ? fill : max(fine, min(fill, 16)));
+  }
   PagedPart r{};
   int before = 0;
-  for (int b0 = 0; b0 < a.c.B; b0 += 64) {
-    const int blocks = b0 + lane < a.c.B ? paged_blocks(a, b0 + lane, BK) : 0;
-    const int parts = b0 + lane < a.c.B ? parts_of(blocks, quota) * units : 0;
-    int incl = parts;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      const int y = __shfl_up(incl, m);
-      if (lane >= m) incl += y;
-    }
-    const uint64_t past = __ballot(before + incl > find);
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const PagedSeq s = b0 == 0 ? head : paged_seq<BK>(a, b0 + lane);
+    const int incl = before + wave_scan(b0 + lane < p.B ? parts_of(s.blocks, quota) * units : 0, 0, add);
+    const uint64_t past = __ballot(incl > find);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
-      const int n = __shfl(blocks, l);
+      const int n = __builtin_amdgcn_readlane(s.blocks, l);
       r.b = b0 + l;
+      r.len = __builtin_amdgcn_readlane(s.len, l);
+      r.n_new = __builtin_amdgcn_readlane(s.n_new, l);
       r.parts = parts_of(n, quota);
-      int i = find - (before + __shfl(incl - parts, l));
+      int i = find - (__builtin_amdgcn_readlane(incl, l) - r.parts * units);
       r.rb = i % a.row_blocks;
       i /= a.row_blocks;
-      const int c = i % r.parts;
+      r.index = i % r.parts;
       r.g = i / r.parts;
-      r.first = (int)((long long)c * n / r.parts);
-      r.last = (int)((long long)(c + 1) * n / r.parts);
+      r.first = (int)((long long)r.index * n / r.parts);
+      r.last = (int)((long long)(r.index + 1) * n / r.parts);
       r.any = true;
       return r;
     }
-    before += __shfl(incl, 63);
+    before = __builtin_amdgcn_readlane(incl, 63);
   }
   return r;
 }
@@ -144,7 +171,7 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 
 // MIXED: some rows of a workgroup may see a key that others do not (several new rows, causal).
 template <int D, int CT, int RT, bool MIXED>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
@@ -152,11 +179,16 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
   __shared__ float lds_ml[kPagedWaves][RT * 16][2];
   const PagedArgs& p = a.c;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
-  const PagedPart part = paged_find<BK>(a, (int)block_id(), lane);
+  const PagedPart part = paged_find<BK>(a, uniform((int)block_id()), lane);
   if (!part.any) return;
-  const int b = uniform(part.b), g = uniform(part.g);
-  const int len = uniform(paged_len(p, b)), n_new = uniform(paged_new(p, b));
+  const int b = uniform(part.b), g = uniform(part.g), len = part.len, n_new = part.n_new;
   const int rows = n_new * p.G, row0 = uniform(part.rb) * (RT * 16);
+  if (a.max_chunks > 1 && part.index == 0 && threadIdx.x == 0) {   // what the join has to know of the unit
+    int32_t* u = a.unit + (((long long)b * p.Hkv + g) * a.row_blocks + part.rb) * 4;
+    u[0] = (int)block_id();
+    u[1] = part.parts;
+    u[2] = rows - row0;
+  }
   if (row0 >= rows) return;
 
   // Query rows: row r is new row r / G, head g G + r % G.
@@ -231,7 +263,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
       const long long row = ((long long)page * p.Hkv + g) * page_rows + (s.pos[h] & (p.R - 1));
       const char* kp = (const char*)p.k_pages + row * (D * CB) + n * (D * CB) + 16 * g4;
 #pragma unroll
-      for (int j = 0; j < NK; ++j) s.k[h][j] = *(const u32x4*)(kp + 64 * j);
+      for (int j = 0; j < NK; ++j) s.k[h][j] = __builtin_nontemporal_load((const u32x4*)(kp + 64 * j));
       const char* vp = (const char*)p.v_pages + row * (D * CB) + g4 * (4 * D * CB);
       // fp32: channels 64 u + 4 n.., u = 0..D/64-1; otherwise E n..
 #pragma unroll
@@ -239,13 +271,13 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         uint32_t* w = s.v[4 * h + j];
         if constexpr (CT == kFp32) {
 #pragma unroll
-          for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = *(const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n);
+          for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = __builtin_nontemporal_load((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
         } else if constexpr (VW == 4) {
-          *(u32x4*)w = *(const u32x4*)(vp + j * (D * CB) + 16 * n);
+          *(u32x4*)w = __builtin_nontemporal_load((const u32x4*)(vp + j * (D * CB) + 16 * n));
         } else if constexpr (VW == 2) {
-          *(u32x2*)w = *(const u32x2*)(vp + j * (D * CB) + 8 * n);
+          *(u32x2*)w = __builtin_nontemporal_load((const u32x2*)(vp + j * (D * CB) + 8 * n));
         } else {
-          *w = *(const uint32_t*)(vp + j * (D * CB) + 4 * n);
+          *w = __builtin_nontemporal_load((const uint32_t*)(vp + j * (D * CB) + 4 * n));
         }
       }
       if constexpr (CT == kFp8) {
@@ -287,9 +319,12 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         for (int w = 0; w < W; ++w) v[j][w] = there ? v[j][w] : 0u;
       }
     }
-    // A key that some rows see and others do not: its value has to stay out of the
-    // others even where it is not finite, which a weight of zero does not achieve.
-    bool odd = false;
+    // A key that some rows see and others do not: its value has to stay out of the others
+    // even where it is not finite, which a weight of zero does not achieve.  Such values are
+    // taken out of the products and go in by themselves: which of the lane's are +inf, -inf
+    // and NaN, a bit each.
+    uint64_t odd[3] = {0, 0, 0};
+    bool any_odd = false;
     if (MIXED && !whole) {
       float z = 0.f;
 #pragma unroll
@@ -303,34 +338,28 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
             z = fmaf(0.f, __uint_as_float(v[j][w] & 0xffff0000u), z);
           }
         }
-      odd = __any(z != z);
-    }
-    // Products of P V: value(j, w) gives dword w of the lane's row j, add(i, x) takes
-    // product i with the accumulator from(i).
-    auto products = [&](const float (&pp)[H][4], auto value, auto from, auto add) {
-      if constexpr (CT == kFp32) {
+      any_odd = __any(z != z);
+      if (any_odd) {
+        auto sort_out = [&](float x, int at) {
+          if (x == INFINITY) odd[0] |= 1ull << at;
+          if (x == -INFINITY) odd[1] |= 1ull << at;
+          if (x != x) odd[2] |= 1ull << at;
+          return fabsf(x) < INFINITY;
+        };
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          f32x4 x = from(i);
+        for (int j = 0; j < VR; ++j)
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            x = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(value(j, i)), pp[0][j], x, 0, 0, 0);
-          add(i, x);
-        }
-      } else {
-        // The weights are rounded to bf16 here, to nearest; their sum l is taken before.
-        const u32x4 pw = {pack_bf16x2(pp[0][0], pp[0][1]), pack_bf16x2(pp[0][2], pp[0][3]),
-                          pack_bf16x2(pp[H - 1][0], pp[H - 1][1]), pack_bf16x2(pp[H - 1][2], pp[H - 1][3])};
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          u32x4 w;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = __builtin_amdgcn_perm(value(2 * j + 1, i / 2), value(2 * j, i / 2), i & 1 ? 0x07060302u : 0x05040100u);
-          add(i, mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), from(i)));
-        }
+          for (int w = 0; w < W; ++w) {
+            if constexpr (CT == kFp32) {
+              if (!sort_out(__uint_as_float(v[j][w]), j * W + w)) v[j][w] = 0u;
+            } else {
+              const bool lo = sort_out(__uint_as_float(v[j][w] << 16), (j * W + w) * 2);
+              const bool hi = sort_out(__uint_as_float(v[j][w] & 0xffff0000u), (j * W + w) * 2 + 1);
+              v[j][w] &= (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
+            }
+          }
       }
-    };
+    }
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
       f32x4 sc[H];
@@ -395,26 +424,56 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
           }
           pr[h][e] = x;
         }
-      if (!MIXED || !odd) {
-        products(pr, [&](int j, int w) { return v[j][w]; }, [&](int i) { return o[t][i]; },
-                 [&](int i, f32x4 x) { o[t][i] = x; });
+      if constexpr (CT == kFp32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int i = 0; i < NT; ++i)
+            o[t][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j][i]), pr[0][j], o[t][i], 0, 0, 0);
       } else {
-        // Row by row: the values that the row sees, its weights, and its sums alone (what a
-        // value that is not finite does to the other rows' is dropped).
-        for (int r = 0; r < 16; ++r) {
-          const int end = __builtin_amdgcn_readlane(lim[t], r);
-          float pp[H][4];
+        // The weights are rounded to bf16 here, to nearest; their sum l is taken before.
+        const u32x4 pw = {pack_bf16x2(pr[0][0], pr[0][1]), pack_bf16x2(pr[0][2], pr[0][3]),
+                          pack_bf16x2(pr[H - 1][0], pr[H - 1][1]), pack_bf16x2(pr[H - 1][2], pr[H - 1][3])};
 #pragma unroll
-          for (int h = 0; h < H; ++h)
+        for (int i = 0; i < NT; ++i) {
+          u32x4 w;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pp[h][e] = n == r ? pr[h][e] : 0.f;
-          products(pp, [&](int j, int w) { return s.pos[j / 4] + 4 * g4 + j % 4 < end ? v[j][w] : 0u; },
-                   [&](int i) { return o[t][i]; },
-                   [&](int i, f32x4 x) {
-#pragma unroll
-                     for (int e = 0; e < 4; ++e) o[t][i][e] = n == r ? x[e] : o[t][i][e];
-                   });
+          for (int j = 0; j < 4; ++j)
+            w[j] = __builtin_amdgcn_perm(v[2 * j + 1][i / 2], v[2 * j][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+          o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), o[t][i]);
         }
+      }
+      if (any_odd) {
+        // How many values of each kind a row sees in a channel, as a product of zeros and ones.
+        float one[H][4];
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) one[h][e] = s.pos[h] + 4 * g4 + e < lim[t] ? 1.f : 0.f;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+          for (int kind = 0; kind < 3; ++kind) {
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (CT == kFp32) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                x = __builtin_amdgcn_mfma_f32_16x16x4f32((odd[kind] >> (j * W + i)) & 1 ? 1.f : 0.f, one[0][j], x, 0, 0, 0);
+            } else {
+              u32x4 w, pw;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                w[j] = ((odd[kind] >> (4 * j * W + i)) & 1 ? 0x3f80u : 0u) |
+                       ((odd[kind] >> ((4 * j + 2) * W + i)) & 1 ? 0x3f800000u : 0u);
+                pw[j] = pack_bf16x2(one[j / 2][2 * (j & 1)], one[j / 2][2 * (j & 1) + 1]);
+              }
+              x = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), x);
+            }
+            const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (x[e] != 0.f) o[t][i][e] += add;
+          }
       }
     }
   };
@@ -493,7 +552,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
           a.ml_part[2 * at + 1] = L;
         }
       } else {
-        const float inv = L == 0.f ? 0.f : 1.0f / L;
+        const float inv = 1.0f / L;
         const int head = g * p.G + r % p.G, nr = r / p.G;
         const long long el = (((long long)b * p.Ln + nr) * p.Hq + head) * D + c0;
 #pragma unroll
@@ -515,29 +574,22 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
 // The join of rows whose keys were cut: o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s in the
 // parts' order.  One workgroup a row; its threads take four channels of every
 // (1024 / D)-th part each, all loads of eight parts in flight, and are joined through LDS.
-template <int BK, int D, bool BF16>
+template <int D, bool BF16>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int T = D / 4, SL = 256 / T, U = 8;   // threads of a row, slices of the parts
   __shared__ f32x4 lds_o[SL][T];
   __shared__ float lds_m[SL], lds_l[SL];
   const PagedArgs& p = a.c;
-  const int lane = threadIdx.x & 63;
   const int rows_all = p.G * p.Ln;
   const long long id = block_id();
   const int r = (int)(id % rows_all);
   const long long bg = id / rows_all;
   const int g = (int)(bg % p.Hkv), b = (int)(bg / p.Hkv);
-  if (b >= p.B || r >= paged_new(p, b) * p.G) return;
-  const int quota = paged_quota<BK>(a, lane);
-  const int parts = parts_of(paged_blocks(a, b, BK), quota);
-  if (parts == 1) return;
-  // The number of the row's first part: all parts of the sequences before, then of the heads before.
-  int before = 0;
-  for (int b0 = 0; b0 < b; b0 += 64)
-    before += wave_sum(b0 + lane < b ? parts_of(paged_blocks(a, b0 + lane, BK), quota) : 0);
-  const int rb = r / kPagedRows;
-  const long long first = ((long long)before * p.Hkv + (long long)g * parts) * a.row_blocks + rb;
-  const int rl = r - rb * kPagedRows;
+  if (b >= p.B) return;
+  const int rb = r / kPagedRows, rl = r - rb * kPagedRows;
+  const int32_t* unit = a.unit + (bg * a.row_blocks + rb) * 4;
+  const int first = unit[0], parts = unit[1];
+  if (parts == 1 || rl >= unit[2]) return;
   const int c = threadIdx.x % T, sl = threadIdx.x / T;
   float M = kNoMax, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -546,7 +598,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
     f32x4 v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const long long at = (first + (long long)min(s0 + u * SL, parts - 1) * a.row_blocks) * a.part_rows + rl;
+      const long long at = ((long long)first + (long long)min(s0 + u * SL, parts - 1) * a.row_blocks) * a.part_rows + rl;
       ms[u] = a.ml_part[2 * at];
       ls[u] = a.ml_part[2 * at + 1];
       v[u] = *(const f32x4*)(a.o_part + at * D + 4 * c);
@@ -606,7 +658,7 @@ hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   else paged_attn_rows<D, CT, 2>(a, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_chunks == 1) return e;
-  hipLaunchKernelGGL((paged_join_kernel<PagedShape<D, CT>::BK, D, CT != kFp32>),
+  hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32>),
                      grid_xy((long long)a.c.B * a.c.Hkv * rows), dim3(256), 0, s, a);
   return hipGetLastError();
 }

@@ -67,11 +67,13 @@ struct PagedAttnArgs {
   float* lse;
   float* o_part;         // [slot][part_rows][D] sums of a workgroup whose keys are a part of its rows'
   float* ml_part;        // [slot][part_rows][2] their maximum (log2 domain) and weight sum
+  int32_t* unit;         // [B][H_kv][row_blocks][4]: a unit's first part, parts and rows
   int row_blocks, part_rows;
-  int target;            // workgroups that the keys of all sequences are cut for
-  int max_chunks;        // at most so many per (sequence, KV head, row block); 1: no parts, no join
+  int max_chunks;        // parts of a unit at most; 1: no parts, no join
   long long grid;
 };
+// Parts that the keys of a ragged batch are cut into at most, besides one for every unit.
+constexpr int kPagedParts = 2048;
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);

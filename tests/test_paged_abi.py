@@ -143,18 +143,18 @@ def test_binding_checks_tensors(lib):
     with pytest.raises(ValueError, match="GPU"):
         _lib.PagedCache(d, k, k, torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
     x = torch.zeros(4, 6, 64)
-    with pytest.raises(ValueError, match="GPU"):
+    with pytest.raises(ValueError, match="on the GPU"):
         _lib.pd_qk_norm_rope(x[:, :4], x[:, 4:], None, None, 0.0, None, 0.0, x[:, :4].clone(), x[:, 4:].clone())
     with pytest.raises(ValueError, match="bf16 or fp32"):
         _lib.pd_qk_norm_rope(x.double(), None, None, None, 0.0, None, 0.0, x.double(), None)
-    types = (torch.float32,)
+    types = torch.float32
     with pytest.raises(ValueError, match="type"):
-        _lib._rows("x", x, x.shape, (torch.bfloat16,))
+        _lib._rows("x", x, x.shape, torch.bfloat16, -1)
     with pytest.raises(ValueError, match="shape"):
-        _lib._rows("x", x, (4, 6, 32), types)
+        _lib._rows("x", x, (4, 6, 32), types, -1)
     with pytest.raises(ValueError, match="heads of a row"):
-        _lib._rows("x", x.transpose(0, 1), (6, 4, 64), types)
+        _lib._rows("x", x.transpose(0, 1), (6, 4, 64), types, -1)
     with pytest.raises(ValueError, match="one stride apart"):
-        _lib._rows("x", torch.zeros(2, 5, 6, 64)[:, :4], (2, 4, 6, 64), types)
+        _lib._rows("x", torch.zeros(2, 5, 6, 64)[:, :4], (2, 4, 6, 64), types, -1)
     with pytest.raises(ValueError, match="contiguous"):
-        _lib._checked("x", torch.zeros(6, 4).t(), (4, 6), types)
+        _lib._checked("x", torch.zeros(6, 4).t(), (4, 6), types, -1)
