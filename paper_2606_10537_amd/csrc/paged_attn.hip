@@ -23,6 +23,8 @@
 //     8 x E block into the A operands of E products.  Row m of product t is channel E m + t.
 // 16x16x4 fp32: k = g, one value a lane; four products per 16-byte read, and the
 // channels of a read are permuted alike in both operands.
+#include <type_traits>
+
 #include "paged_common.h"
 
 namespace pd {
@@ -169,9 +171,8 @@ __device__ __forceinline__ float group_sum(float x) {
 
 constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 
-// MIXED: some rows of a workgroup may see a key that others do not (several new rows, causal).
-template <int D, int CT, int RT, bool MIXED>
-__global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+template <int D, int CT, int RT>
+__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
@@ -230,7 +231,9 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
   // Where the keys of 64 steps lie, a lane each: page and position of every 16.
   const int32_t* table = p.page_table + (long long)b * p.max_pages;
   const int32_t* chosen = a.page_idx ? a.page_idx + ((long long)b * p.Hkv + g) * a.top_k : nullptr;
-  const int n_steps = part.last - part.first;
+  // Blocks behind the last row's own position are in no row's sight.
+  const int sight = p.causal ? len - n_new + 1 + min(rows - 1, row0 + RT * 16 - 1) / p.G : len;
+  const int n_steps = (chosen ? part.last : min(part.last, (max(sight, 0) + BK - 1) / BK)) - part.first;
   int at_page[H], at_pos[H];
   bool bad = false;
   auto locate = [&](int i0) {
@@ -287,13 +290,9 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
     }
   };
 
-  auto compute = [&](PagedStep<D, CT>& s) {
-    bool whole = true, inside = true;
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      whole = whole && s.pos[h] + 16 <= every;     // every row sees every key
-      inside = inside && s.pos[h] + 16 <= len;     // every key is there
-    }
+  // whole: every row sees every key of the step.
+  auto compute = [&](PagedStep<D, CT>& s, auto whole_step) {
+    constexpr bool whole = decltype(whole_step)::value;
     // Values as bf16 (or fp32), zeros where no key is: a weight of zero does not cancel
     // an infinity or a NaN.
     constexpr int W = CT == kFp32 ? VW : D / 32;
@@ -311,7 +310,7 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
         for (int w = 0; w < W; ++w) v[j][w] = s.v[j][w];
       }
     }
-    if (!inside) {
+    if constexpr (!whole) {
 #pragma unroll
       for (int j = 0; j < VR; ++j) {
         const bool there = s.pos[j / 4] + 4 * g4 + j % 4 < len;
@@ -325,7 +324,7 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
     // and NaN, a bit each.
     uint64_t odd[3] = {0, 0, 0};
     bool any_odd = false;
-    if (MIXED && !whole) {
+    if (!whole && p.causal && n_new > 1) {
       float z = 0.f;
 #pragma unroll
       for (int j = 0; j < VR; ++j)
@@ -443,7 +442,7 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
           o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), o[t][i]);
         }
       }
-      if (any_odd) {
+      if (!whole && any_odd) {
         // How many values of each kind a row sees in a channel, as a product of zeros and ones.
         float one[H][4];
 #pragma unroll
@@ -478,25 +477,45 @@ __global__ __launch_bounds__(256, RT == 1 && !MIXED ? 2 : 1) void paged_attn_ker
     }
   };
 
+  // Whole steps first, the next one's loads in flight; from the first other one on (the end
+  // of the rows, the new rows' own positions) step by step, with masks.
+  auto whole_at = [&](int i) {
+    bool w = true;
+#pragma unroll
+    for (int h = 0; h < H; ++h) w = w && __builtin_amdgcn_readlane(at_pos[h], i & 63) + 16 <= every;
+    return w;
+  };
   if (n_steps > 0) {
     PagedStep<D, CT> s0, s1;
+    int i = 0;
+    auto next = [&](PagedStep<D, CT>& s) {   // step i + 1, if there is one; whether it is whole
+      if (i + 1 >= n_steps) return false;
+      if (((i + 1) & 63) == 0) locate(i + 1);
+      load(s, i + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      return whole_at(i + 1);
+    };
     locate(0);
     load(s0, 0);
-    for (int i = 0;;) {
-      if (i + 1 < n_steps) {
-        if (((i + 1) & 63) == 0) locate(i + 1);
-        load(s1, i + 1);
-        __builtin_amdgcn_sched_barrier(0);
+    bool whole = whole_at(0);
+    while (whole) {
+      whole = next(s1);
+      compute(s0, std::true_type{});
+      ++i;
+      if (!whole) {
+        s0 = s1;
+        break;
       }
-      compute(s0);
-      if (++i >= n_steps) break;
-      if (i + 1 < n_steps) {
-        if (((i + 1) & 63) == 0) locate(i + 1);
-        load(s0, i + 1);
-        __builtin_amdgcn_sched_barrier(0);
+      whole = next(s0);
+      compute(s1, std::true_type{});
+      ++i;
+    }
+    while (i < n_steps) {
+      compute(s0, std::false_type{});
+      if (++i < n_steps) {
+        if ((i & 63) == 0) locate(i);
+        load(s0, i);
       }
-      compute(s1);
-      if (++i >= n_steps) break;
     }
   }
 
@@ -645,17 +664,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   if (c == 0 && a.lse) a.lse[((long long)b * p.Hq + head) * p.Ln + nr] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
 }
 
-template <int D, int CT, int RT>
-void paged_attn_rows(const PagedAttnArgs& a, hipStream_t s) {
-  if (a.c.causal && a.c.Ln > 1) hipLaunchKernelGGL((paged_attn_kernel<D, CT, RT, true>), grid_xy(a.grid), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, RT, false>), grid_xy(a.grid), dim3(256), 0, s, a);
-}
-
 template <int D, int CT>
 hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
+  const dim3 grid = grid_xy(a.grid);
   const int rows = a.c.G * a.c.Ln;
-  if (rows <= 16) paged_attn_rows<D, CT, 1>(a, s);
-  else paged_attn_rows<D, CT, 2>(a, s);
+  if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_chunks == 1) return e;
   hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32>),
