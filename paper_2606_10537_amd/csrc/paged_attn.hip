@@ -39,6 +39,7 @@ struct PagedPart {
   int len, n_new;        // the sequence's rows and new rows
   int first, last;       // blocks of keys of this part
   int parts, index;      // how many the row block's keys are cut into, and which this is
+  int slot;              // where its sums go; a unit's parts lie row_blocks apart
   bool any;
 };
 
@@ -59,7 +60,7 @@ __device__ __forceinline__ int wave_scan(int x, int none, F op) {
 
 // The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
 // units (KV head x row block).  With a quota of Q blocks a part, a unit has ceil(n_b / Q)
-// parts of nearly one size; they are numbered by sequence, head, part, row block.  Every
+// parts of nearly one size; they are numbered by sequence, head and part.  Every
 // wave finds its own part from the lengths, 64 sequences at a time.
 //
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
@@ -120,11 +121,21 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       r.len = __builtin_amdgcn_readlane(s.len, l);
       r.n_new = __builtin_amdgcn_readlane(s.n_new, l);
       r.parts = parts_of(n, quota);
-      int i = find - (__builtin_amdgcn_readlane(incl, l) - r.parts * units);
-      r.rb = i % a.row_blocks;
-      i /= a.row_blocks;
-      r.index = i % r.parts;
-      r.g = i / r.parts;
+      const int base = __builtin_amdgcn_readlane(incl, l) - r.parts * units;
+      // Row blocks of the same keys run on one XCD, eight workgroups apart, so that all but
+      // the first find them in its L2.
+      const int i = find - base, pairs = p.Hkv * r.parts, full = pairs / kNumXcd * kNumXcd * a.row_blocks;
+      int pair;
+      if (i < full) {
+        pair = i / (kNumXcd * a.row_blocks) * kNumXcd + i % kNumXcd;
+        r.rb = i / kNumXcd % a.row_blocks;
+      } else {
+        pair = i / a.row_blocks;
+        r.rb = i % a.row_blocks;
+      }
+      r.slot = base + pair * a.row_blocks + r.rb;
+      r.index = pair % r.parts;
+      r.g = pair / r.parts;
       r.first = (int)((long long)r.index * n / r.parts);
       r.last = (int)((long long)(r.index + 1) * n / r.parts);
       r.any = true;
@@ -169,9 +180,17 @@ __device__ __forceinline__ float group_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
+template <bool STREAM, class T>
+__device__ __forceinline__ T fetch(const T* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 
-template <int D, int CT, int RT>
+// STREAM: the keys are read by one workgroup alone (non-temporal loads: 8 x 32K keys 654
+// against 718 us); row blocks that share them leave them in the caches.
+template <int D, int CT, int RT, bool STREAM>
 __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
@@ -186,7 +205,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
   const int rows = n_new * p.G, row0 = uniform(part.rb) * (RT * 16);
   if (a.max_chunks > 1 && part.index == 0 && threadIdx.x == 0) {   // what the join has to know of the unit
     int32_t* u = a.unit + (((long long)b * p.Hkv + g) * a.row_blocks + part.rb) * 4;
-    u[0] = (int)block_id();
+    u[0] = part.slot;
     u[1] = part.parts;
     u[2] = rows - row0;
   }
@@ -266,7 +285,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
       const long long row = ((long long)page * p.Hkv + g) * page_rows + (s.pos[h] & (p.R - 1));
       const char* kp = (const char*)p.k_pages + row * (D * CB) + n * (D * CB) + 16 * g4;
 #pragma unroll
-      for (int j = 0; j < NK; ++j) s.k[h][j] = __builtin_nontemporal_load((const u32x4*)(kp + 64 * j));
+      for (int j = 0; j < NK; ++j) s.k[h][j] = fetch<STREAM>((const u32x4*)(kp + 64 * j));
       const char* vp = (const char*)p.v_pages + row * (D * CB) + g4 * (4 * D * CB);
       // fp32: channels 64 u + 4 n.., u = 0..D/64-1; otherwise E n..
 #pragma unroll
@@ -274,13 +293,13 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         uint32_t* w = s.v[4 * h + j];
         if constexpr (CT == kFp32) {
 #pragma unroll
-          for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = __builtin_nontemporal_load((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
+          for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
         } else if constexpr (VW == 4) {
-          *(u32x4*)w = __builtin_nontemporal_load((const u32x4*)(vp + j * (D * CB) + 16 * n));
+          *(u32x4*)w = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 16 * n));
         } else if constexpr (VW == 2) {
-          *(u32x2*)w = __builtin_nontemporal_load((const u32x2*)(vp + j * (D * CB) + 8 * n));
+          *(u32x2*)w = fetch<STREAM>((const u32x2*)(vp + j * (D * CB) + 8 * n));
         } else {
-          *w = __builtin_nontemporal_load((const uint32_t*)(vp + j * (D * CB) + 4 * n));
+          *w = fetch<STREAM>((const uint32_t*)(vp + j * (D * CB) + 4 * n));
         }
       }
       if constexpr (CT == kFp8) {
@@ -532,7 +551,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
   }
   __syncthreads();
   const int rl = threadIdx.x >> 4, c0 = (threadIdx.x & 15) * (D / 16);
-  const long long slot = (long long)block_id() * a.part_rows;
+  const long long slot = (long long)part.slot * a.part_rows;
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     float top = lds_ml[0][t * 16 + n][0];
@@ -668,8 +687,9 @@ template <int D, int CT>
 hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   const dim3 grid = grid_xy(a.grid);
   const int rows = a.c.G * a.c.Ln;
-  if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2>), grid, dim3(256), 0, s, a);
+  if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1, true>), grid, dim3(256), 0, s, a);
+  else if (rows <= kPagedRows) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, false>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_chunks == 1) return e;
   hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32>),
