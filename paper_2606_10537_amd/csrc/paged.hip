@@ -361,152 +361,200 @@ hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s) {
 // product of two bf16 is exact there, and a sum of d of them too unless their
 // exponents lie more than 30 apart.  The bounds are read once per block of query rows
 // and converted once; memory bounds it for few query rows (16 lanes or more read a
-// page's bounds in whole lines), the double FMAs (one per element and row) for many.
+// page's bounds in whole lines, a lane four pages at once: 512 pages of 8 x 32 heads 12.9 us,
+// one page at a time 18.7), the double FMAs (one per element and row) for many.
+
+// x + the same of the lane that `ctrl` names.
+template <int CTRL>
+__device__ __forceinline__ double add_dpp(double x) {
+  const u32x2 w = __builtin_bit_cast(u32x2, x);
+  const u32x2 y = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xf, 0xf, true),
+                   (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xf, 0xf, true)};
+  return x + __builtin_bit_cast(double, y);
+}
+// Sum over groups of L neighbouring lanes, the same bits in each.
+template <int L>
+__device__ __forceinline__ double lanes_sum(double x) {
+  x = add_dpp<0xb1>(x);                            // quad_perm [1,0,3,2]
+  x = add_dpp<0x4e>(x);                            // quad_perm [2,3,0,1]
+  x = add_dpp<0x141>(x);                           // row_half_mirror
+  if constexpr (L >= 16) x = add_dpp<0x140>(x);    // row_mirror
+  if constexpr (L >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
+constexpr int kScoreTurns = 4;   // pages of a lane
 template <bool BF16, int D>
-__global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a, int blocks) {
-  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = 256 / L, EB = BF16 ? 2 : 4, QR = 16;
+__global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = 256 / L, EB = BF16 ? 2 : 4, QR = 16, U = kScoreTurns;
   __shared__ __align__(16) float q[QR][D];
   const PagedArgs& p = a.c;
-  const long long id = block_id();
-  const long long bh = id / blocks;
-  const int b = (int)(bh / p.Hkv), g = (int)(bh % p.Hkv);
+  const int id = uniform((int)block_id());
+  const int bh = a.by_blocks.quot(id);
+  const int b = a.by_heads.quot(bh), g = a.by_heads.rem(bh, b);
   if (b >= p.B) return;
   const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
   const int rows = paged_new(p, b) * p.G;
-  const int j0 = (int)(id % blocks) * PP, c = threadIdx.x % L;
+  const int j0 = a.by_blocks.rem(id, bh) * PP * U, c = threadIdx.x % L;
   if (j0 >= pages) return;
-  const int j = j0 + threadIdx.x / L;
-  int page = p.page_table[(long long)b * p.max_pages + min(j, pages - 1)];
-  const bool bad = (unsigned)page >= (unsigned)p.n_pages;
-  if (bad) page = 0;
-  const char* src = (const char*)p.k_bounds + (((long long)page * p.Hkv + g) * 2 * D + c * E) * EB;
-  Row16<BF16> lo, hi;
-  lo.load(src);
-  hi.load(src + D * EB);
-  float l32[E], h32[E];
-  lo.unpack(l32);
-  hi.unpack(h32);
-  double best = -INFINITY;
-  bool nan = bad;
+  Row16<BF16> lo[U], hi[U];
+  bool nan[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int j = min(j0 + u * PP + (int)threadIdx.x / L, pages - 1);
+    int page = p.page_table[(long long)b * p.max_pages + j];
+    nan[u] = (unsigned)page >= (unsigned)p.n_pages;
+    if (nan[u]) page = 0;
+    const char* src = (const char*)p.k_bounds + (((long long)page * p.Hkv + g) * 2 * D + c * E) * EB;
+    lo[u].load(src);
+    hi[u].load(src + D * EB);
+  }
+  double best[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) best[u] = -INFINITY;
   for (int r0 = 0; r0 < rows; r0 += QR) {
     const int n = min(QR, rows - r0);
     __syncthreads();
     for (int i = threadIdx.x; i < n * L; i += 256) {
-      const int r = r0 + i / L, ch = i % L;
+      const int r = r0 + i / L, ch = i % L, nr = a.by_group.quot(r);
       Row16<BF16> x;
       x.load((const char*)a.q +
-             ((((long long)b * p.Ln + r / p.G) * p.Hq + (long long)g * p.G + r % p.G) * D + ch * E) * EB);
+             ((((long long)b * p.Ln + nr) * p.Hq + (long long)g * p.G + a.by_group.rem(r, nr)) * D + ch * E) * EB);
       x.unpack(&q[i / L][ch * E]);
     }
     __syncthreads();
     for (int r = 0; r < n; ++r) {
-      double s = 0.0;
+      float x[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float x = q[r][c * E + e];
-        s = fma((double)x, (double)(x >= 0.f ? h32[e] : l32[e]), s);
+      for (int e = 0; e < E; ++e) x[e] = q[r][c * E + e];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float l32[E], h32[E];
+        lo[u].unpack(l32);
+        hi[u].unpack(h32);
+        double s = 0.0;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = fma((double)x[e], (double)(x[e] >= 0.f ? h32[e] : l32[e]), s);
+        s = lanes_sum<L>(s);
+        nan[u] = nan[u] || s != s;
+        best[u] = fmax(best[u], s);
       }
-#pragma unroll
-      for (int m = 1; m < L; m *= 2) s += __shfl_xor(s, m);
-      nan = nan || s != s;
-      best = fmax(best, s);
     }
   }
-  if (c == 0 && j < pages) a.score[bh * p.max_pages + j] = nan ? (double)NAN : best;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int j = j0 + u * PP + threadIdx.x / L;
+    if (c == 0 && j < pages) a.score[(long long)bh * p.max_pages + j] = nan[u] ? (double)NAN : best[u];
+  }
 }
 
 // The top_k pages of one (sequence, KV head), ascending.  Scores map to 64-bit keys whose
-// order is theirs; a radix descent of eight bits a pass finds the key of the last page
-// kept, then the pages above it and the lowest ones equal to it are written in order.
-// The latency of those passes bounds it: a thread keeps its keys in registers for up
-// to KPT pages and reads them again from the workspace beyond.
-constexpr int kSelectThreads = 512;
+// order is theirs; a radix descent of eight bits a pass, from the highest bit in which
+// the keys differ down to the first digit that parts exactly the pages wanted, finds the
+// least key kept.  Then the pages above it, and the lowest of those equal to it, are
+// written in order.  The latency of the passes bounds it (2048 pages 7.0 us; eight
+// passes over all 64 bits 13.5): a thread keeps its pages, neighbours, in registers for up to
+// KPT of them (KPT = 0: reads them again from the workspace).
+constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
 
-__device__ __forceinline__ uint64_t page_key(const PageSelectArgs& a, const double* score, int j, int pages) {
-  if (j < a.n_first || j >= pages - a.n_last) return ~0ull;
-  const double s = score[j];
-  if (s != s) return ~0ull - 1;
+__device__ __forceinline__ uint64_t page_key(double s) {
+  if (s != s) return ~0ull;
   const uint64_t u = __builtin_bit_cast(uint64_t, s == 0.0 ? 0.0 : s);
   return (u >> 63) ? ~u : (u | (1ull << 63));
 }
 
-// Exclusive sum over the workgroup of one value per thread; total: the sum of all.
-__device__ __forceinline__ int block_prefix(int x, int* lds, int* total) {
+// Exclusive sum over the workgroup of one value per thread.
+__device__ __forceinline__ int block_prefix(int x, int* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int s = x;
+  const int incl = wave_scan(x, 0, [](int p, int q) { return p + q; });
+  if (lane == 63) lds[wave] = incl;
+  __syncthreads();
+  int before = 0;
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const int y = __shfl_up(s, m);
-    if (lane >= m) s += y;
-  }
-  __syncthreads();
-  if (lane == 63) lds[wave] = s;
-  __syncthreads();
-  int before = 0, all = 0;
-  for (int w = 0; w < kSelectThreads / 64; ++w) {
-    if (w < wave) before += lds[w];
-    all += lds[w];
-  }
-  *total = all;
-  return before + s - x;
+  for (int w = 0; w < kSelectWaves - 1; ++w) before += w < wave ? lds[w] : 0;
+  return before + incl - x;
 }
 
 template <int KPT>
 __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectArgs a) {
   __shared__ uint32_t hist[256];
-  __shared__ int sums[kSelectThreads / 64];
-  __shared__ int pick[2];
+  __shared__ uint64_t all_or[kSelectWaves], all_and[kSelectWaves];
+  __shared__ int sums[2][kSelectWaves], pick[3];
   const PagedArgs& p = a.c;
-  const long long bh = block_id();
-  const int b = (int)(bh / p.Hkv), tid = threadIdx.x;
+  const int bh = uniform((int)block_id()), b = a.by_heads.quot(bh), tid = threadIdx.x;
   if (b >= p.B) return;
   const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
-  const double* score = a.score + bh * p.max_pages;
-  int32_t* out = a.page_idx + bh * a.top_k;
+  const double* score = a.score + (long long)bh * p.max_pages;
+  int32_t* out = a.page_idx + (long long)bh * a.top_k;
   const int k = min(a.top_k, pages);
   for (int i = k + tid; i < a.top_k; i += kSelectThreads) out[i] = -1;
-  if (k == pages) {
-    for (int i = tid; i < k; i += kSelectThreads) out[i] = i;
+  // Forced pages: 0..head-1 and tail..pages-1.
+  const int head = min(a.n_first, pages), tail = max(head, pages - a.n_last), forced = head + pages - tail;
+  if (k == pages || forced >= k) {
+    for (int i = tid; i < k; i += kSelectThreads) out[i] = i < head ? i : k == pages ? i : tail + i - head;
     return;
   }
-  uint64_t key[KPT];
-  const int turns = (pages + kSelectThreads - 1) / kSelectThreads;
+  int need = k - forced;                // pages still to be taken among those that match the prefix
+  const int per = (pages + kSelectThreads - 1) / kSelectThreads, j0 = tid * per;
+  uint64_t key[KPT > 0 ? KPT : 1];
 #pragma unroll
-  for (int t = 0; t < KPT; ++t)
-    key[t] = t * kSelectThreads + tid < pages ? page_key(a, score, t * kSelectThreads + tid, pages) : 0;
-  auto key_of = [&](int t) {   // t beyond the registers: pages there are many of
-    return t * kSelectThreads + tid < pages ? page_key(a, score, t * kSelectThreads + tid, pages) : 0;
+  for (int t = 0; t < KPT; ++t) key[t] = t < per && j0 + t < pages ? page_key(score[j0 + t]) : 0;
+  auto free_page = [&](int j) { return j >= head && j < tail; };
+  auto each = [&](auto f) {             // f(page, key) for the thread's pages that are not forced
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int t = 0; t < KPT; ++t)
+        if (t < per && free_page(j0 + t)) f(j0 + t, key[t]);
+    } else {
+      for (int t = 0; t < per; ++t)
+        if (free_page(j0 + t)) f(j0 + t, page_key(score[j0 + t]));
+    }
   };
-  uint64_t prefix = 0;
-  int need = k;                // pages still to be taken among those that match the prefix
-  for (int shift = 56; shift >= 0; shift -= 8) {
+  uint64_t any = 0, every = ~0ull;
+  each([&](int, uint64_t x) {
+    any |= x;
+    every &= x;
+  });
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    any |= __shfl_xor(any, m);
+    every &= __shfl_xor(every, m);
+  }
+  if ((tid & 63) == 0) {
+    all_or[tid >> 6] = any;
+    all_and[tid >> 6] = every;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kSelectWaves; ++w) {
+    any |= all_or[w];
+    every &= all_and[w];
+  }
+  // Bits below `low` are still open.
+  int low = any == every ? 0 : 64 - __clzll((long long)(any ^ every));
+  uint64_t prefix = low >= 64 ? 0 : any >> low << low;
+  bool exact = false;                   // all pages from the prefix up are kept
+  while (low > 0 && !exact) {
+    const int shift = max(low - 8, 0);
+    const uint32_t digits = (1u << (low - shift)) - 1;
     for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
     __syncthreads();
-    auto count = [&](uint64_t x, int j) {
-      if (j < pages && (shift == 56 || (x >> (shift + 8)) == (prefix >> (shift + 8))))
-        atomicAdd(&hist[(x >> shift) & 255], 1u);
-    };
-#pragma unroll
-    for (int t = 0; t < KPT; ++t) count(key[t], t * kSelectThreads + tid);
-    for (int t = KPT; t < turns; ++t) count(key_of(t), t * kSelectThreads + tid);
+    each([&](int, uint64_t x) {
+      if (low >= 64 || (x >> low) == (prefix >> low)) atomicAdd(&hist[(uint32_t)(x >> shift) & digits], 1u);
+    });
     __syncthreads();
     if (tid < 64) {
       // Lane l owns digits 255-4l .. 252-4l, the highest first.
       int own[4], s = 0;
 #pragma unroll
       for (int i = 0; i < 4; ++i) s += own[i] = (int)hist[255 - 4 * tid - i];
-      int incl = s;
-#pragma unroll
-      for (int m = 1; m < 64; m *= 2) {
-        const int y = __shfl_up(incl, m);
-        if (tid >= m) incl += y;
-      }
-      int before = incl - s;
+      int before = wave_scan(s, 0, [](int x, int y) { return x + y; }) - s;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (before < need && before + own[i] >= need) {
           pick[0] = 255 - 4 * tid - i;
           pick[1] = before;
+          pick[2] = own[i];
         }
         before += own[i];
       }
@@ -514,47 +562,52 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectA
     __syncthreads();
     prefix |= (uint64_t)pick[0] << shift;
     need -= pick[1];
-    __syncthreads();
+    exact = pick[2] == need;
+    low = shift;
   }
-  // prefix: the key of the last page kept; need: how many pages with that key are.
-  int written = 0, equal = 0;
-  for (int t = 0; t < turns; ++t) {
-    const int j = t * kSelectThreads + tid;
-    uint64_t x = 0;
-    if (t < KPT) {
-#pragma unroll
-      for (int i = 0; i < KPT; ++i)
-        if (i == t) x = key[i];
-    } else {
-      x = key_of(t);
-    }
-    int total;
-    const int same = j < pages && x == prefix;
-    const int rank = equal + block_prefix(same, sums, &total);
-    equal += total;
-    const int keep = j < pages && (x > prefix || (same && rank < need));
-    const int at = written + block_prefix(keep, sums, &total);
-    written += total;
-    if (keep) out[at] = j;
+  // Of the pages with the prefix's own key, all, or the lowest `need`.
+  int rank = 0;
+  if (!exact) {
+    int same = 0;
+    each([&](int, uint64_t x) { same += x == prefix; });
+    rank = block_prefix(same, sums[0]);
   }
+  int kept = 0, r = rank;
+  auto keep = [&](uint64_t x) { return x > prefix || (x == prefix && (exact || r++ < need)); };
+  each([&](int, uint64_t x) { kept += keep(x); });
+  int at = block_prefix(kept, sums[1]) + head;
+  r = rank;
+  each([&](int j, uint64_t x) {
+    if (keep(x)) out[at++] = j;
+  });
+  for (int i = tid; i < forced; i += kSelectThreads) {
+    if (i < head) out[i] = i;
+    else out[k - forced + i] = tail + i - head;
+  }
+}
+
+int page_score_blocks(const PagedArgs& p) {
+  const int per = 256 / (p.D / (p.bf16 ? 8 : 4)) * kScoreTurns;
+  return (p.max_pages + per - 1) / per;
 }
 
 hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s) {
   const PagedArgs& p = a.c;
-  const int per = 256 / (p.D / (p.bf16 ? 8 : 4)), blocks = (p.max_pages + per - 1) / per;
-  const dim3 grid = grid_xy((long long)p.B * p.Hkv * blocks);
+  const dim3 grid = grid_xy((long long)p.B * p.Hkv * page_score_blocks(p));
   if (p.bf16) {
-    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<true, 128>), grid, dim3(256), 0, s, a, blocks);
-    else hipLaunchKernelGGL((page_score_kernel<true, 64>), grid, dim3(256), 0, s, a, blocks);
+    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<true, 128>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((page_score_kernel<true, 64>), grid, dim3(256), 0, s, a);
   } else {
-    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<false, 128>), grid, dim3(256), 0, s, a, blocks);
-    else hipLaunchKernelGGL((page_score_kernel<false, 64>), grid, dim3(256), 0, s, a, blocks);
+    if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<false, 128>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((page_score_kernel<false, 64>), grid, dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 sg = grid_xy((long long)p.B * p.Hkv);
   if (p.max_pages <= kSelectThreads) hipLaunchKernelGGL(page_select_kernel<1>, sg, dim3(kSelectThreads), 0, s, a);
-  else hipLaunchKernelGGL(page_select_kernel<8>, sg, dim3(kSelectThreads), 0, s, a);
+  else if (p.max_pages <= 4 * kSelectThreads) hipLaunchKernelGGL(page_select_kernel<4>, sg, dim3(kSelectThreads), 0, s, a);
+  else if (p.max_pages <= 16 * kSelectThreads) hipLaunchKernelGGL(page_select_kernel<16>, sg, dim3(kSelectThreads), 0, s, a);
+  else hipLaunchKernelGGL(page_select_kernel<0>, sg, dim3(kSelectThreads), 0, s, a);
   return hipGetLastError();
 }
 

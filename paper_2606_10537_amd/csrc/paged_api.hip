@@ -277,6 +277,9 @@ pd_status pd_paged_select(const pd_paged_dims* d, const pd_paged_cache* cache, c
   a.n_last = n_last;
   a.page_idx = page_idx;
   a.score = (double*)workspace;
+  a.by_group = pd::fast_div(a.c.G);
+  a.by_heads = pd::fast_div(a.c.Hkv);
+  a.by_blocks = pd::fast_div(pd::page_score_blocks(a.c));
   return hip_status(pd::launch_paged_select(a, (hipStream_t)stream), "page selection kernels");
 }
 
@@ -305,6 +308,10 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.part_rows = plan.part_rows;
   a.max_chunks = plan.max_chunks;
   a.grid = plan.grid;
+  a.by_group = pd::fast_div(a.c.G);
+  a.by_heads = pd::fast_div(a.c.Hkv);
+  a.by_rows = pd::fast_div(a.c.G * a.c.Ln);
+  a.by_blocks = pd::fast_div(a.row_blocks);
   return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");
 }
 

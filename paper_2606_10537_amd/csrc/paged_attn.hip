@@ -43,21 +43,6 @@ struct PagedPart {
   bool any;
 };
 
-// Sum (inclusive) and maximum over the lanes up to each, on the vector units: 16 lanes at a
-// time, then the last lane of each row handed on.
-template <class F>
-__device__ __forceinline__ int wave_scan(int x, int none, F op) {
-#define PD_SCAN(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(none, x, ctrl, rows, 0xf, false))
-  PD_SCAN(0x111, 0xf);   // row_shr:1
-  PD_SCAN(0x112, 0xf);
-  PD_SCAN(0x114, 0xf);
-  PD_SCAN(0x118, 0xf);
-  PD_SCAN(0x142, 0xa);   // row_bcast:15
-  PD_SCAN(0x143, 0xc);   // row_bcast:31
-#undef PD_SCAN
-  return x;
-}
-
 // The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
 // units (KV head x row block).  With a quota of Q blocks a part, a unit has ceil(n_b / Q)
 // parts of nearly one size; they are numbered by sequence, head and part.  Every
@@ -75,12 +60,11 @@ struct PagedSeq {
 template <int BK>
 __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int b) {
   const PagedArgs& p = a.c;
-  PagedSeq s{0, 0, 0};
-  if (b < p.B) {
-    s.len = paged_len(p, b);
-    s.n_new = paged_new(p, b);
-    if (s.len > 0 && s.n_new > 0) s.blocks = ((a.page_idx ? a.top_k << p.log2R : s.len) + BK - 1) / BK;
-  }
+  // Both loads in flight at once, also where there is no such sequence.
+  const int at = b < p.B ? b : 0;
+  const int len = p.kv_len[at], n_new = p.new_rows ? p.new_rows[at] : p.Ln;
+  PagedSeq s{min(max(len, 0), p.max_pages << p.log2R), min(max(n_new, 0), p.Ln), 0};
+  if (b < p.B && s.len > 0 && s.n_new > 0) s.blocks = ((a.page_idx ? a.top_k << p.log2R : s.len) + BK - 1) / BK;
   return s;
 }
 
@@ -125,19 +109,30 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       // Row blocks of the same keys run on one XCD, eight workgroups apart, so that all but
       // the first find them in its L2.
       const int i = find - base, pairs = p.Hkv * r.parts, full = pairs / kNumXcd * kNumXcd * a.row_blocks;
-      int pair;
-      if (i < full) {
-        pair = i / (kNumXcd * a.row_blocks) * kNumXcd + i % kNumXcd;
-        r.rb = i / kNumXcd % a.row_blocks;
-      } else {
-        pair = i / a.row_blocks;
-        r.rb = i % a.row_blocks;
+      int pair = i;
+      r.rb = 0;
+      if (a.row_blocks > 1) {
+        if (i < full) {
+          const int q = a.by_blocks.quot(i / kNumXcd);
+          r.rb = a.by_blocks.rem(i / kNumXcd, q);
+          pair = q * kNumXcd + i % kNumXcd;
+        } else {
+          pair = a.by_blocks.quot(i);
+          r.rb = a.by_blocks.rem(i, pair);
+        }
       }
       r.slot = base + pair * a.row_blocks + r.rb;
-      r.index = pair % r.parts;
-      r.g = pair / r.parts;
-      r.first = (int)((long long)r.index * n / r.parts);
-      r.last = (int)((long long)(r.index + 1) * n / r.parts);
+      r.index = 0;
+      r.g = pair;
+      r.first = 0;
+      r.last = n;
+      if (r.parts > 1) {
+        r.g = pair / r.parts;
+        r.index = pair - r.g * r.parts;
+        const int each = n / r.parts, more = n - each * r.parts;   // the first `more` parts take a block more
+        r.first = r.index * each + min(r.index, more);
+        r.last = r.first + each + (r.index < more ? 1 : 0);
+      }
       r.any = true;
       return r;
     }
@@ -220,9 +215,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
   for (int t = 0; t < RT; ++t) {
     const int r = row0 + t * 16 + n;
     const bool real = r < rows;
-    const int rr = real ? r : row0;
-    const long long q_el = (((long long)b * p.Ln + rr / p.G) * p.Hq + (long long)g * p.G + rr % p.G) * D;
-    lim[t] = !real ? 0 : p.causal ? len - n_new + 1 + r / p.G : len;
+    const int rr = real ? r : row0, nr = a.by_group.quot(rr);
+    const long long q_el = (((long long)b * p.Ln + nr) * p.Hq + (long long)g * p.G + a.by_group.rem(rr, nr)) * D;
+    lim[t] = !real ? 0 : p.causal ? len - n_new + 1 + nr : len;
     if constexpr (CT == kFp32) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) qf[t][i] = *(const f32x4*)((const float*)a.q + q_el + 16 * i + 4 * g4);
@@ -235,7 +230,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
       }
     }
   }
-  every = p.causal ? len - n_new + 1 + row0 / p.G : len;
+  every = p.causal ? len - n_new + 1 + a.by_group.quot(row0) : len;
 
   f32x4 o[RT][NT];
   float m[RT], l[RT];
@@ -251,7 +246,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
   const int32_t* table = p.page_table + (long long)b * p.max_pages;
   const int32_t* chosen = a.page_idx ? a.page_idx + ((long long)b * p.Hkv + g) * a.top_k : nullptr;
   // Blocks behind the last row's own position are in no row's sight.
-  const int sight = p.causal ? len - n_new + 1 + min(rows - 1, row0 + RT * 16 - 1) / p.G : len;
+  const int sight = p.causal ? len - n_new + 1 + a.by_group.quot(min(rows - 1, row0 + RT * 16 - 1)) : len;
   const int n_steps = (chosen ? part.last : min(part.last, (max(sight, 0) + BK - 1) / BK)) - part.first;
   int at_page[H], at_pos[H];
   bool bad = false;
@@ -591,7 +586,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         }
       } else {
         const float inv = 1.0f / L;
-        const int head = g * p.G + r % p.G, nr = r / p.G;
+        const int nr = a.by_group.quot(r), head = g * p.G + a.by_group.rem(r, nr);
         const long long el = (((long long)b * p.Ln + nr) * p.Hq + head) * D + c0;
 #pragma unroll
         for (int e = 0; e < D / 16; e += 4) {
@@ -618,14 +613,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   __shared__ f32x4 lds_o[SL][T];
   __shared__ float lds_m[SL], lds_l[SL];
   const PagedArgs& p = a.c;
-  const int rows_all = p.G * p.Ln;
-  const long long id = block_id();
-  const int r = (int)(id % rows_all);
-  const long long bg = id / rows_all;
-  const int g = (int)(bg % p.Hkv), b = (int)(bg / p.Hkv);
+  const int id = uniform((int)block_id());
+  const int bg = a.by_rows.quot(id), r = a.by_rows.rem(id, bg);
+  const int b = a.by_heads.quot(bg), g = a.by_heads.rem(bg, b);
   if (b >= p.B) return;
   const int rb = r / kPagedRows, rl = r - rb * kPagedRows;
-  const int32_t* unit = a.unit + (bg * a.row_blocks + rb) * 4;
+  const int32_t* unit = a.unit + ((long long)bg * a.row_blocks + rb) * 4;
   const int first = unit[0], parts = unit[1];
   if (parts == 1 || rl >= unit[2]) return;
   const int c = threadIdx.x % T, sl = threadIdx.x / T;
@@ -673,7 +666,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
     L += w * lds_l[s];
     acc += w * lds_o[s][c];
   }
-  const int head = g * p.G + r % p.G, nr = r / p.G;
+  const int nr = a.by_group.quot(r), head = g * p.G + a.by_group.rem(r, nr);
   const long long el = (((long long)b * p.Ln + nr) * p.Hq + head) * D + 4 * c;
   const float inv = 1.0f / L;
 #pragma unroll

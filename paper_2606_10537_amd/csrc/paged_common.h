@@ -47,4 +47,19 @@ __device__ __forceinline__ int paged_new(const PagedArgs& p, int b) {
   return p.new_rows ? min(max(p.new_rows[b], 0), p.Ln) : p.Ln;
 }
 
+// Inclusive scan over the wave (sums, maxima), on the vector units: 16 lanes at a time, then
+// the last lane of each row handed on.
+template <class F>
+__device__ __forceinline__ int wave_scan(int x, int none, F op) {
+#define PD_SCAN(ctrl, rows) x = op(x, __builtin_amdgcn_update_dpp(none, x, ctrl, rows, 0xf, false))
+  PD_SCAN(0x111, 0xf);   // row_shr:1
+  PD_SCAN(0x112, 0xf);
+  PD_SCAN(0x114, 0xf);
+  PD_SCAN(0x118, 0xf);
+  PD_SCAN(0x142, 0xa);   // row_bcast:15
+  PD_SCAN(0x143, 0xc);   // row_bcast:31
+#undef PD_SCAN
+  return x;
+}
+
 }  // namespace pd

@@ -5,6 +5,22 @@
 
 namespace pd {
 
+// Division of n < 2^31 by a divisor known on the host: n * mul >> shift with
+// shift = 31 + ceil(log2 d) and mul = ceil(2^shift / d), which is too large by less than
+// n / 2^shift < 1 / d and so never reaches the next quotient.
+struct FastDiv {
+  uint32_t mul, shift, d;
+#ifdef __HIPCC__
+  __device__ __forceinline__ int quot(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+  __device__ __forceinline__ int rem(int n, int q) const { return n - q * (int)d; }
+#endif
+};
+inline FastDiv fast_div(int d) {
+  uint32_t log2 = 0;
+  while ((1ll << log2) < d) ++log2;
+  return FastDiv{(uint32_t)(((1ull << (31 + log2)) + (uint32_t)d - 1) / (uint32_t)d), 31 + log2, (uint32_t)d};
+}
+
 struct NormRopeArgs {
   const void *x[2];      // query rows, key rows
   void *y[2];
@@ -51,7 +67,9 @@ struct PageSelectArgs {
   int top_k, n_first, n_last;
   int32_t* page_idx;
   double* score;         // [B][H_kv][max_pages] workspace
+  FastDiv by_group, by_heads, by_blocks;   // G, H_kv, workgroups of a (sequence, head)
 };
+int page_score_blocks(const PagedArgs& p);   // workgroups that score the pages of one (sequence, head)
 hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s);
 
 // Rows of one query block: the query rows of a (sequence, KV head) are taken in
@@ -71,6 +89,7 @@ struct PagedAttnArgs {
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   long long grid;
+  FastDiv by_group, by_heads, by_rows, by_blocks;  // G, H_kv, G * L_n, row_blocks
 };
 // Parts that the keys of a ragged batch are cut into at most, besides one for every unit.
 constexpr int kPagedParts = 2048;

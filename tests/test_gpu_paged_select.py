@@ -73,7 +73,7 @@ def raw_select(score_rows, k, first=0, last=0, seed=0):
     return out[:, 0].cpu().numpy()
 
 
-@pytest.mark.parametrize("n", [1, 2, 511, 512, 513, 4096, 4097, 9000])
+@pytest.mark.parametrize("n", [1, 2, 511, 512, 513, 2048, 2049, 4097, 8192, 9000])
 def test_ties_and_special_scores(gpu_lib, n):
     """Equal scores (all, or in long runs), signed zeros, infinities and NaN, over one and several turns of the threads
     and beyond the registers."""
