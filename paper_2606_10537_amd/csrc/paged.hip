@@ -20,8 +20,10 @@ namespace pd {
 // each pair and wave, not one for each head.  Lanes 0..d/2-1 take a pair each and
 // hand the sines and cosines over through LDS.
 //
-// U: head groups a wave loads before it uses the first.
-template <bool BF16, int D, int U>
+// U: head groups a wave loads before it uses the first.  STREAM: loads and stores past the
+// caches, for calls beyond what these hold (32768 rows of 64 heads 191 us, 210 without; a 4096-row
+// call of 40 heads 20.4 and 21.0, and there the reader finds the rows in the caches).
+template <bool BF16, int D, int U, bool STREAM>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int groups) {
   constexpr int E = BF16 ? 8 : 4;       // elements of a lane
   constexpr int L = D / E;              // lanes of a head
@@ -42,8 +44,9 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int g
     const long long el = (long long)(t ? h - a.Hq : h) * D + c * E;
     src[u] = (const char*)(t ? a.x[1] : a.x[0]) + (row * (t ? a.xs[1] : a.xs[0]) + el) * (BF16 ? 2 : 4);
     dst[u] = (char*)(t ? a.y[1] : a.y[0]) + (row * (t ? a.ys[1] : a.ys[0]) + el) * (BF16 ? 2 : 4);
-    if (h < H) x[u].load(src[u]);
-    else x[u].zero();
+    if (h >= H) x[u].zero();
+    else if constexpr (STREAM) x[u].load_once(src[u]);
+    else x[u].load(src[u]);
   }
   float cs[E], sn[E];
   if (a.pos) {
@@ -78,9 +81,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int g
       float s = 0.f;
 #pragma unroll
       for (int e = 0; e < E; ++e) s = fmaf(y[e], y[e], s);
-#pragma unroll
-      for (int m = 1; m < L; m *= 2) s += __shfl_xor(s, m);
-      const float r = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
+      const float r = 1.0f / sqrtf(lanes_sum<L>(s) * (1.0f / D) + a.eps);
       float w[E], w1[E];
       wv[0].unpack(w);
       wv[1].unpack(w1);
@@ -94,26 +95,43 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int g
     if (a.pos) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float p = __shfl_xor(y[e], L / 2);
-        y[e] = fmaf(p, sn[e], y[e] * cs[e]);
+        y[e] = fmaf(partner<L>(y[e]), sn[e], y[e] * cs[e]);
       }
     }
     x[u].pack(y);
-    if (h < H) x[u].store(dst[u]);
+    if (h < H) {
+      if constexpr (STREAM) x[u].store_once(dst[u]);
+      else x[u].store(dst[u]);
+    }
   }
 }
 
 template <bool BF16, int D>
 hipError_t norm_rope_of(const NormRopeArgs& a, hipStream_t s) {
   constexpr int HP = 64 / (D / (BF16 ? 8 : 4));
-  const int H = a.Hq + a.Hkv;
-  // Four head groups a wave keep enough loads in flight where the rows fill the CUs;
+  const int H = a.Hq + a.Hkv, all = (H + HP - 1) / HP;   // head groups of a row
+  // Up to five head groups a wave, the row's groups shared evenly among its waves, keep
+  // enough loads in flight and compute a row's angles seldom (H = 40, d = 64: 81 us with
+  // waves of 32 and 8 heads, 60 with one of 40) where that leaves eight waves for every CU;
   // below that every group is a wave of its own.
-  const bool wide = a.rows * ((H + 4 * HP - 1) / (4 * HP)) >= 8 * 256;
-  const int per = wide ? 4 * HP : HP, groups = (H + per - 1) / per;
+  const int waves = (all + 4) / 5;
+  const bool wide = a.rows * waves >= 8 * kNumCu;
+  const int U = wide ? (all + waves - 1) / waves : 1, groups = (all + U - 1) / U;
   const dim3 grid = grid_xy((a.rows * groups + 3) / 4);
-  if (wide) hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, 4>), grid, dim3(256), 0, s, a, groups);
-  else hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, 1>), grid, dim3(256), 0, s, a, groups);
+  const bool stream = (double)a.rows * H * D * (BF16 ? 4 : 8) >= 256e6;   // what the last cache holds
+#define PD_NORM(N)                                                                                                  \
+  case N:                                                                                                           \
+    if (stream) hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, true>), grid, dim3(256), 0, s, a, groups);      \
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, false>), grid, dim3(256), 0, s, a, groups);            \
+    break
+  switch (U) {
+    PD_NORM(1);
+    PD_NORM(2);
+    PD_NORM(3);
+    PD_NORM(4);
+    PD_NORM(5);
+  }
+#undef PD_NORM
   return hipGetLastError();
 }
 
@@ -127,29 +145,35 @@ hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s) {
 //
 // One workgroup per (sequence, page that new rows fall into, KV head): the bounds of a
 // page need all its rows, and so no atomics are needed.  A lane holds 16 bytes
-// of a row as in the norm kernel; waves 0 and 2 take the key rows, 1 and 3 the
-// value rows.  Memory bounds it: every new row is read once and written once.
+// of a row as in the norm kernel; even waves take the key rows, odd ones the value
+// rows.  Memory bounds it: every new row is read once and written once.  A single
+// token is one chain of loads: the lengths, then the row and the page's number, then the
+// old bounds.
 //
 // Quantisation: e from the bits of the largest magnitude (448 = 1.75 * 2^8, so e is the
 // binary exponent minus 8, or one more where the mantissa exceeds 1.75), the
 // product with 2^-e is exact, and the conversion rounds to nearest even.
-template <bool BF16, bool FP8, int D>
-__global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
+//
+// NW: waves.  Eight where a page may take more than 64 new rows (pages of 256 rows, one head,
+// 4000 rows: 12.5 us, 16.2 with four, 11.9 with sixteen, which take 80 instead of 51 us for
+// prompts of four sequences of 32 heads over pages of 128 rows).
+template <bool BF16, bool FP8, int D, int NW>
+__global__ __launch_bounds__(NW * 64) void paged_append_kernel(AppendArgs a) {
   constexpr int E = BF16 ? 8 : 4, L = D / E, HP = 64 / L, EB = BF16 ? 2 : 4;
-  __shared__ float bound[2][2][D];
+  __shared__ float bound[NW / 2][2][D];
   const PagedArgs& p = a.c;
-  const long long id = block_id();
-  const int h = (int)(id % p.Hkv);
-  const long long bj = id / p.Hkv;
-  const int b = (int)(bj / a.pages);
+  const int id = uniform((int)block_id());
+  const int bj = a.by_heads.quot(id), h = a.by_heads.rem(id, bj);
+  const int b = a.by_pages.quot(bj);
   if (b >= p.B) return;
   const int len = paged_len(p, b), n_new = paged_new(p, b);
   const int start = len - n_new;                       // position of new row 0; below 0: rows that are not written
-  const int j = (max(start, 0) >> p.log2R) + (int)(bj % a.pages);
+  const int j = (max(start, 0) >> p.log2R) + a.by_pages.rem(bj, b);
   const int lo = max(max(start, 0), j << p.log2R), hi = min(len, (j + 1) << p.log2R);
   if (lo >= hi) return;
-  const int page = p.page_table[(long long)b * p.max_pages + j];
-  if ((unsigned)page >= (unsigned)p.n_pages) return;
+  const int number = p.page_table[(long long)b * p.max_pages + j];
+  const bool there = (unsigned)number < (unsigned)p.n_pages;
+  const int page = there ? number : 0;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % L;
   const int kv = wave & 1;
   const char* src = (const char*)(kv ? a.v_new : a.k_new) + ((long long)h * D + c * E) * EB;
@@ -158,6 +182,15 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
   char* dst = (char*)(kv ? p.v_pages : p.k_pages) + (base * D + c * E) * (FP8 ? 1 : EB);
   uint8_t* ex = FP8 ? (kv ? p.v_exp : p.k_exp) + base : nullptr;
   const bool bounds = p.k_bounds && kv == 0;
+  const bool widen = (lo & (p.R - 1)) != 0;            // the page's row 0 is an older one
+  // This thread's element of the bounds: the least keys, then the largest.
+  const int bi = threadIdx.x;
+  const long long bat = ((long long)page * p.Hkv + h) * 2 * D + bi;
+  float old = 0.f;
+  if (p.k_bounds && widen && bi < 2 * D) {
+    if constexpr (BF16) old = bf16_to_f32(((const uint16_t*)p.k_bounds)[bat]);
+    else old = ((const float*)p.k_bounds)[bat];
+  }
   float least[E], most[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
@@ -165,17 +198,17 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     most[e] = -INFINITY;
   }
   constexpr int U = 4;   // rows of a lane in flight
-  for (int r0 = lo + (wave >> 1) * HP * U; r0 < hi; r0 += 2 * HP * U) {
+  for (int r0 = lo + (wave >> 1) * HP * U; r0 < hi; r0 += NW / 2 * HP * U) {
     Row16<BF16> x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = min(r0 + u * HP + lane / L, hi - 1);
-      x[u].load(src + ((long long)b * p.Ln + (r - start)) * stride);
+      x[u].load_once(src + ((long long)b * p.Ln + (r - start)) * stride);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int r = r0 + u * HP + lane / L;
-      const bool live = r < hi;
+      const bool live = r < hi && there;
       const int slot = r & (p.R - 1);
       float y[E];
       x[u].unpack(y);
@@ -193,8 +226,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
           const float t = fabsf(y[e]);
           m = fmaxf(m, t < INFINITY ? t : 0.f);
         }
-#pragma unroll
-        for (int k = 1; k < L; k *= 2) m = fmaxf(m, __shfl_xor(m, k));
+        m = lanes_max<L>(m);
         const uint32_t bits = __float_as_uint(m);
         const int e2 = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
         const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
@@ -215,7 +247,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
           if (c == 0) ex[slot] = (uint8_t)(e2 + 127);
         }
       } else {
-        if (live) x[u].store(dst + (long long)slot * D * EB);
+        if (live) x[u].store_once(dst + (long long)slot * D * EB);
       }
     }
   }
@@ -235,34 +267,33 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * D; i += 256) {
-    const bool up = i >= D;
-    const int ch = up ? i - D : i;
-    float x = bound[0][up][ch];
-    x = up ? fmaxf(x, bound[1][up][ch]) : fminf(x, bound[1][up][ch]);
-    const long long at = ((long long)page * p.Hkv + h) * 2 * D + i;
-    if constexpr (BF16) {
-      uint16_t* q = (uint16_t*)p.k_bounds + at;
-      if ((lo & (p.R - 1)) != 0) x = up ? fmaxf(x, bf16_to_f32(*q)) : fminf(x, bf16_to_f32(*q));
-      *q = f32_to_bf16(x);
-    } else {
-      float* q = (float*)p.k_bounds + at;
-      if ((lo & (p.R - 1)) != 0) x = up ? fmaxf(x, *q) : fminf(x, *q);
-      *q = x;
-    }
-  }
+  if (bi >= 2 * D || !there) return;
+  const bool up = bi >= D;
+  const int ch = up ? bi - D : bi;
+  float x = widen ? old : up ? -INFINITY : INFINITY;
+#pragma unroll
+  for (int w = 0; w < NW / 2; ++w) x = up ? fmaxf(x, bound[w][1][ch]) : fminf(x, bound[w][0][ch]);
+  if constexpr (BF16) ((uint16_t*)p.k_bounds)[bat] = f32_to_bf16(x);
+  else ((float*)p.k_bounds)[bat] = x;
 }
 
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
   const dim3 grid = grid_xy((long long)a.c.B * a.pages * a.c.Hkv);
-#define PD_APPEND(BF, F8)                                                                                \
-  do {                                                                                                   \
-    if (a.c.D == 128) hipLaunchKernelGGL((paged_append_kernel<BF, F8, 128>), grid, dim3(256), 0, s, a);  \
-    else hipLaunchKernelGGL((paged_append_kernel<BF, F8, 64>), grid, dim3(256), 0, s, a);                \
+  const bool tall = a.c.R > 64 && a.c.Ln > 64;
+#define PD_APPEND(BF, F8, DD)                                                                              \
+  do {                                                                                                     \
+    if (tall) hipLaunchKernelGGL((paged_append_kernel<BF, F8, DD, 8>), grid, dim3(512), 0, s, a);        \
+    else hipLaunchKernelGGL((paged_append_kernel<BF, F8, DD, 4>), grid, dim3(256), 0, s, a);               \
   } while (0)
-  if (a.c.fp8) PD_APPEND(true, true);
-  else if (a.c.bf16) PD_APPEND(true, false);
-  else PD_APPEND(false, false);
+  if (a.c.D == 128) {
+    if (a.c.fp8) PD_APPEND(true, true, 128);
+    else if (a.c.bf16) PD_APPEND(true, false, 128);
+    else PD_APPEND(false, false, 128);
+  } else {
+    if (a.c.fp8) PD_APPEND(true, true, 64);
+    else if (a.c.bf16) PD_APPEND(true, false, 64);
+    else PD_APPEND(false, false, 64);
+  }
 #undef PD_APPEND
   return hipGetLastError();
 }
@@ -272,17 +303,17 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
 // rows of one (sequence, head), which lie beside each other in the pages too.
 // Memory bounds it.
 template <bool BF16, bool FP8, int D>
-__global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int blocks) {
+__global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a) {
   constexpr int E = BF16 ? 8 : 4, L = D / E, RP = 256 / L, EB = BF16 ? 2 : 4, U = 4;
   const PagedArgs& p = a.c;
-  const long long id = block_id();
-  const long long bh = id / blocks;
-  const int b = (int)(bh / p.Hkv), h = (int)(bh % p.Hkv);
+  const int id = uniform((int)block_id());
+  const int bh = a.by_blocks.quot(id), block = a.by_blocks.rem(id, bh);
+  const int b = a.by_heads.quot(bh), h = a.by_heads.rem(bh, b);
   if (b >= p.B) return;
   const int len = paged_len(p, b), c = threadIdx.x % L;
-  const int row0 = (int)(id % blocks) * RP * U + threadIdx.x / L;
+  const int row0 = block * RP * U + threadIdx.x / L;
   const int end = min(len - a.first, a.n);
-  if ((int)(id % blocks) * RP * U >= end) return;
+  if (block * RP * U >= end) return;
   const int32_t* table = p.page_table + (long long)b * p.max_pages;
   long long at[U];
   bool bad[U];
@@ -297,14 +328,14 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int blocks)
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     const char* src = (const char*)(kv ? p.v_pages : p.k_pages);
-    char* out = (char*)(kv ? a.v_out : a.k_out) + (bh * a.n * D + c * E) * EB;
+    char* out = (char*)(kv ? a.v_out : a.k_out) + ((long long)bh * a.n * D + c * E) * EB;
     if constexpr (FP8) {
       const uint8_t* ex = kv ? p.v_exp : p.k_exp;
       u32x2 w[U];
       float s[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        w[u] = *(const u32x2*)(src + at[u] * D + c * E);
+        w[u] = __builtin_nontemporal_load((const u32x2*)(src + at[u] * D + c * E));
         s[u] = exp_to_scale(ex[at[u]]);
       }
 #pragma unroll
@@ -322,27 +353,27 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a, int blocks)
         Row16<true> x;
         x.pack(y);
         if (bad[u]) x.nan();
-        if (row0 + u * RP < end) x.store(out + (long long)(row0 + u * RP) * D * EB);
+        if (row0 + u * RP < end) x.store_once(out + (long long)(row0 + u * RP) * D * EB);
       }
     } else {
       Row16<BF16> x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u].load(src + (at[u] * D + c * E) * EB);
+      for (int u = 0; u < U; ++u) x[u].load_once(src + (at[u] * D + c * E) * EB);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (bad[u]) x[u].nan();
-        if (row0 + u * RP < end) x[u].store(out + (long long)(row0 + u * RP) * D * EB);
+        if (row0 + u * RP < end) x[u].store_once(out + (long long)(row0 + u * RP) * D * EB);
       }
     }
   }
 }
 
 template <bool BF16, bool FP8, int D>
-hipError_t read_of(const ReadArgs& a, hipStream_t s) {
+hipError_t read_of(ReadArgs a, hipStream_t s) {
   constexpr int rows = 256 / (D / (BF16 ? 8 : 4)) * 4;
   const int blocks = (a.n + rows - 1) / rows;
-  hipLaunchKernelGGL((paged_read_kernel<BF16, FP8, D>), grid_xy((long long)a.c.B * a.c.Hkv * blocks), dim3(256), 0,
-                     s, a, blocks);
+  a.by_blocks = fast_div(blocks);
+  hipLaunchKernelGGL((paged_read_kernel<BF16, FP8, D>), grid_xy((long long)a.c.B * a.c.Hkv * blocks), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

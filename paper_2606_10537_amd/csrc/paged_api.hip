@@ -235,6 +235,8 @@ pd_status pd_paged_append(const pd_paged_dims* d, const pd_paged_cache* cache, c
   a.ks = k_stride;
   a.vs = v_stride;
   a.pages = (int)touched_pages(d);
+  a.by_heads = pd::fast_div(a.c.Hkv);
+  a.by_pages = pd::fast_div(a.pages);
   return hip_status(pd::launch_paged_append(a, (hipStream_t)stream), "append kernel");
 }
 
@@ -255,6 +257,7 @@ pd_status pd_paged_read(const pd_paged_dims* d, const pd_paged_cache* cache, int
   a.v_out = v_out;
   a.first = first;
   a.n = n_rows;
+  a.by_heads = pd::fast_div(a.c.Hkv);
   return hip_status(pd::launch_paged_read(a, (hipStream_t)stream), "read-back kernel");
 }
 

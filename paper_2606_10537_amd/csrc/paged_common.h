@@ -14,6 +14,9 @@ struct Row16 {
   u32x4 v;
   __device__ __forceinline__ void load(const void* p) { v = *(const u32x4*)p; }
   __device__ __forceinline__ void store(void* p) const { *(u32x4*)p = v; }
+  // Data that is read or written once, past the caches where it can.
+  __device__ __forceinline__ void load_once(const void* p) { v = __builtin_nontemporal_load((const u32x4*)p); }
+  __device__ __forceinline__ void store_once(void* p) const { __builtin_nontemporal_store(v, (u32x4*)p); }
   __device__ __forceinline__ void zero() { v = u32x4{0, 0, 0, 0}; }
   __device__ __forceinline__ void nan() { v = u32x4{kNanWord, kNanWord, kNanWord, kNanWord}; }
   __device__ __forceinline__ void unpack(float* y) const {
@@ -59,6 +62,45 @@ __device__ __forceinline__ int wave_scan(int x, int none, F op) {
   PD_SCAN(0x142, 0xa);   // row_bcast:15
   PD_SCAN(0x143, 0xc);   // row_bcast:31
 #undef PD_SCAN
+  return x;
+}
+
+// The value of the lane that a DPP control names (all lanes active, none out of range).
+template <int CTRL, int BANKS = 0xf>
+__device__ __forceinline__ float dpp(float old, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), CTRL, 0xf, BANKS, false));
+}
+// The value of lane ^ L / 2, for groups of L = 8, 16 or 32 neighbouring lanes.
+template <int L>
+__device__ __forceinline__ float partner(float x) {
+  if constexpr (L == 8) {
+    // lanes 4..7 of every eight from four below, lanes 0..3 from four above
+    return dpp<0x104, 0x5>(dpp<0x114, 0xa>(x, x), x);
+  } else if constexpr (L == 16) {
+    return dpp<0x128>(x, x);   // row_ror:8
+  } else {
+    return __shfl_xor(x, L / 2);
+  }
+}
+// Sum over groups of L neighbouring lanes, the same bits in each.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float x) {
+  x += dpp<0xb1>(x, x);                            // quad_perm [1,0,3,2]
+  x += dpp<0x4e>(x, x);                            // quad_perm [2,3,0,1]
+  x += dpp<0x141>(x, x);                           // row_half_mirror
+  if constexpr (L >= 16) x += dpp<0x140>(x, x);    // row_mirror
+  if constexpr (L >= 32) x += __shfl_xor(x, 16);
+  return x;
+}
+
+// Maximum over groups of L neighbouring lanes.
+template <int L>
+__device__ __forceinline__ float lanes_max(float x) {
+  x = fmaxf(x, dpp<0xb1>(x, x));
+  x = fmaxf(x, dpp<0x4e>(x, x));
+  x = fmaxf(x, dpp<0x141>(x, x));
+  if constexpr (L >= 16) x = fmaxf(x, dpp<0x140>(x, x));
+  if constexpr (L >= 32) x = fmaxf(x, __shfl_xor(x, 16));
   return x;
 }
 

@@ -51,6 +51,7 @@ struct AppendArgs {
   const void *k_new, *v_new;
   long long ks, vs;      // row strides, elements
   int pages;             // pages that the new rows of one sequence can touch
+  FastDiv by_heads, by_pages;
 };
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
 
@@ -58,6 +59,7 @@ struct ReadArgs {
   PagedArgs c;
   void *k_out, *v_out;
   int first, n;
+  FastDiv by_heads, by_blocks;   // H_kv, workgroups of a (sequence, head)
 };
 hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s);
 
