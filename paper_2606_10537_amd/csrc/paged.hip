@@ -24,16 +24,16 @@ namespace pd {
 // caches, for calls beyond what these hold (32768 rows of 64 heads 191 us, 210 without; a 4096-row
 // call of 40 heads 20.4 and 21.0, and there the reader finds the rows in the caches).
 template <bool BF16, int D, int U, bool STREAM>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int groups) {
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   constexpr int E = BF16 ? 8 : 4;       // elements of a lane
   constexpr int L = D / E;              // lanes of a head
   constexpr int HP = 64 / L;            // heads of a wave
   __shared__ float2 table[4][D / 2];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, c = lane % L;
-  const long long item = (long long)block_id() * 4 + wave;
-  const long long row = item / groups;
+  const int item = uniform((int)block_id() * 4 + wave), at = a.by_groups.quot(item);
+  const long long row = at;
   if (row >= a.rows) return;
-  const int h0 = (int)(item - row * groups) * HP * U + lane / L, H = a.Hq + a.Hkv;
+  const int h0 = a.by_groups.rem(item, at) * HP * U + lane / L, H = a.Hq + a.Hkv;
   const char* src[U];
   char* dst[U];
   Row16<BF16> x[U];
@@ -107,7 +107,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a, int g
 }
 
 template <bool BF16, int D>
-hipError_t norm_rope_of(const NormRopeArgs& a, hipStream_t s) {
+hipError_t norm_rope_of(NormRopeArgs a, hipStream_t s) {
   constexpr int HP = 64 / (D / (BF16 ? 8 : 4));
   const int H = a.Hq + a.Hkv, all = (H + HP - 1) / HP;   // head groups of a row
   // Up to five head groups a wave, the row's groups shared evenly among its waves, keep
@@ -117,12 +117,13 @@ hipError_t norm_rope_of(const NormRopeArgs& a, hipStream_t s) {
   const int waves = (all + 4) / 5;
   const bool wide = a.rows * waves >= 8 * kNumCu;
   const int U = wide ? (all + waves - 1) / waves : 1, groups = (all + U - 1) / U;
+  a.by_groups = fast_div(groups);
   const dim3 grid = grid_xy((a.rows * groups + 3) / 4);
   const bool stream = (double)a.rows * H * D * (BF16 ? 4 : 8) >= 256e6;   // what the last cache holds
 #define PD_NORM(N)                                                                                                  \
   case N:                                                                                                           \
-    if (stream) hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, true>), grid, dim3(256), 0, s, a, groups);      \
-    else hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, false>), grid, dim3(256), 0, s, a, groups);            \
+    if (stream) hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, true>), grid, dim3(256), 0, s, a);      \
+    else hipLaunchKernelGGL((qk_norm_rope_kernel<BF16, D, N, false>), grid, dim3(256), 0, s, a);            \
     break
   switch (U) {
     PD_NORM(1);

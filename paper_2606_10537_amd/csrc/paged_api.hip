@@ -176,6 +176,10 @@ pd_status pd_qk_norm_rope(int32_t n_rows, int32_t n_heads_q, int32_t n_heads_kv,
   if (!std::isfinite(eps) || eps < 0.f) return fail(PD_ERR_BAD_DIMS, "eps must be finite and >= 0");
   if (!std::isfinite(rope_base) || rope_base < 0.0)
     return fail(PD_ERR_BAD_DIMS, "rope_base must be finite and >= 0 (0: no rotation)");
+  // A wave takes at least two heads (fp32, d = 128).
+  if ((double)n_rows * ((n_heads_q + (long long)n_heads_kv + 1) / 2) >= 2147483640.0)
+    return fail(PD_ERR_BAD_DIMS, "n_rows=%d rows of %lld heads are too large for one launch", n_rows,
+                n_heads_q + (long long)n_heads_kv);
   if (n_rows == 0) return ok();
   const int eb = dtype == PD_BF16 ? 2 : 4;
   if (n_heads_q > 0) {

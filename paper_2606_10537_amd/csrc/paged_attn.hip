@@ -89,7 +89,8 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
     const long long seqs = (long long)p.B * units;
     all *= units;
     const bool even = 4 * most * seqs <= 5 * all && seqs <= 2 * kNumCu;
-    const int fill = (int)((all + kNumCu - 1) / kNumCu), fine = (int)((all + kPagedParts - 1) / kPagedParts);
+    const int fill = (int)min((all + kNumCu - 1) / kNumCu, 1ll << 30);
+    const int fine = (int)min((all + kPagedParts - 1) / kPagedParts, 1ll << 30);
     quota = max(1, even ? fill : max(fine, min(fill, 16)));
   }
   PagedPart r{};

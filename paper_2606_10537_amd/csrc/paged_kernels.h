@@ -32,6 +32,7 @@ struct NormRopeArgs {
   float eps;
   double log2_step;      // log2(rope_base) * 2 / d: pair i turns by pos * 2^(-i * log2_step)
   bool bf16;
+  FastDiv by_groups;     // waves of a row
 };
 hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s);
 

@@ -120,6 +120,7 @@ def norm(lib, T=4, hq=4, hkv=2, d=64, dt=PD_BF16, q=A, qs=256, k=A, ks=128, wq=A
 
 def test_norm_refusals(lib):
     assert norm(lib, T=-1) == DIMS and norm(lib, hq=-1) == DIMS and norm(lib, hq=0, hkv=0) == DIMS
+    assert norm(lib, T=(1 << 31) - 1, hq=4, hkv=2) == DIMS
     assert norm(lib, d=32) == UNSUP and norm(lib, dt=PD_FP8_E4M3) == UNSUP
     assert norm(lib, eps=-1.0) == DIMS and norm(lib, eps=math.nan) == DIMS
     assert norm(lib, base=-1.0) == DIMS and norm(lib, base=math.inf) == DIMS
