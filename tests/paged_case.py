@@ -147,5 +147,5 @@ def check_attn(case, o, lse, page_idx=None, fill=7.0):
             if lse is not None:
                 gl = lse[b, g * G:(g + 1) * G, :m].T.reshape(-1)
                 tl = delta[:, 0] + 2.0 ** -21 * (1 + np.abs(np.where(np.isfinite(l), l, 0)))
-                ok = np.where(np.isfinite(l), np.abs(gl - l) <= tl, gl == l)
+                ok = (gl == l) | (np.isfinite(l) & (np.abs(gl - np.where(np.isfinite(l), l, 0)) <= tl))
                 assert ok.all(), (b, g, gl[~ok][:3], l[~ok][:3])
