@@ -45,7 +45,7 @@ struct PagedPart {
 
 // The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
 // units (KV head x row block).  With a quota of Q blocks a part, a unit has ceil(n_b / Q)
-// parts of nearly one size; they are numbered by sequence, head and part.  Every
+// parts, the last one shorter; they are numbered by sequence, head and part.  Every
 // wave finds its own part from the lengths, 64 sequences at a time.
 //
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
@@ -68,7 +68,18 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ int parts_of(int blocks, int quota) { return blocks <= quota ? 1 : (blocks + quota - 1) / quota; }
+// n / d for 0 <= n < 2^27 and quotients below 2^17: the product with the reciprocal is off by
+// less than one then.
+__device__ __forceinline__ int short_div(int n, int d) {
+  int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d));
+  const int r = n - q * d;
+  q += r >= d ? 1 : 0;
+  return r < 0 ? q - 1 : q;
+}
+// ceil(blocks / quota), at most kPagedParts + 1.
+__device__ __forceinline__ int parts_of(int blocks, int quota) {
+  return blocks <= quota ? 1 : short_div(blocks - 1, quota) + 1;
+}
 
 template <int BK>
 __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find, int lane) {
@@ -79,19 +90,24 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   const PagedSeq head = paged_seq<BK>(a, lane);
   int quota = 1 << 30;
   if (a.max_chunks > 1) {
-    long long all = 0;
+    // In fp32, which a quota need not be exact for: an error of 2^-12 in it still leaves the
+    // number of parts below what the host has made room for.
+    float all = 0.f;
     int most = 0;
     for (int b0 = 0; b0 < p.B; b0 += 64) {
       const int n = b0 == 0 ? head.blocks : paged_seq<BK>(a, b0 + lane).blocks;
-      all += __builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
+      all += (float)__builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
       most = max(most, __builtin_amdgcn_readlane(wave_scan(n, 0, larger), 63));
     }
-    const long long seqs = (long long)p.B * units;
-    all *= units;
-    const bool even = 4 * most * seqs <= 5 * all && seqs <= 2 * kNumCu;
-    const int fill = (int)min((all + kNumCu - 1) / kNumCu, 1ll << 30);
-    const int fine = (int)min((all + kPagedParts - 1) / kPagedParts, 1ll << 30);
-    quota = max(1, even ? fill : max(fine, min(fill, 16)));
+    const float seqs = (float)p.B * (float)units;
+    all *= (float)units;
+    auto ceil_of = [](float x) {
+      const int c = (int)fminf(x, 1073741824.f);
+      return (float)c < x ? c + 1 : c;
+    };
+    const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * (1.f / kPagedParts));
+    const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
+    quota = max(1, uniform(even ? fill : max(fine, min(fill, 16))));
   }
   PagedPart r{};
   int before = 0;
@@ -109,11 +125,11 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       const int base = __builtin_amdgcn_readlane(incl, l) - r.parts * units;
       // Row blocks of the same keys run on one XCD, eight workgroups apart, so that all but
       // the first find them in its L2.
-      const int i = find - base, pairs = p.Hkv * r.parts, full = pairs / kNumXcd * kNumXcd * a.row_blocks;
+      const int i = find - base;
       int pair = i;
       r.rb = 0;
       if (a.row_blocks > 1) {
-        if (i < full) {
+        if (i < p.Hkv * r.parts / kNumXcd * kNumXcd * a.row_blocks) {
           const int q = a.by_blocks.quot(i / kNumXcd);
           r.rb = a.by_blocks.rem(i / kNumXcd, q);
           pair = q * kNumXcd + i % kNumXcd;
@@ -128,11 +144,10 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       r.first = 0;
       r.last = n;
       if (r.parts > 1) {
-        r.g = pair / r.parts;
+        r.g = short_div(pair, r.parts);
         r.index = pair - r.g * r.parts;
-        const int each = n / r.parts, more = n - each * r.parts;   // the first `more` parts take a block more
-        r.first = r.index * each + min(r.index, more);
-        r.last = r.first + each + (r.index < more ? 1 : 0);
+        r.first = r.index * quota;
+        r.last = min(r.first + quota, n);
       }
       r.any = true;
       return r;
