@@ -416,19 +416,13 @@ __device__ __forceinline__ double lanes_sum(double x) {
 }
 
 constexpr int kScoreTurns = 4;   // pages of a lane
-template <bool BF16, int D>
-__global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
-  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = 256 / L, EB = BF16 ? 2 : 4, QR = 16, U = kScoreTurns;
-  __shared__ __align__(16) float q[QR][D];
+// Scores of pages j0 .. of (b, g), four pages a lane of NT threads; put(j, score).
+template <bool BF16, int D, int NT, class F>
+__device__ __forceinline__ void score_pages(const PageSelectArgs& a, int b, int g, int j0, int pages, int rows,
+                                            float (&q)[16][D], F put) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = NT / L, EB = BF16 ? 2 : 4, QR = 16, U = kScoreTurns;
   const PagedArgs& p = a.c;
-  const int id = uniform((int)block_id());
-  const int bh = a.by_blocks.quot(id);
-  const int b = a.by_heads.quot(bh), g = a.by_heads.rem(bh, b);
-  if (b >= p.B) return;
-  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
-  const int rows = paged_new(p, b) * p.G;
-  const int j0 = a.by_blocks.rem(id, bh) * PP * U, c = threadIdx.x % L;
-  if (j0 >= pages) return;
+  const int c = threadIdx.x % L;
   Row16<BF16> lo[U], hi[U];
   bool nan[U];
 #pragma unroll
@@ -447,7 +441,7 @@ __global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
   for (int r0 = 0; r0 < rows; r0 += QR) {
     const int n = min(QR, rows - r0);
     __syncthreads();
-    for (int i = threadIdx.x; i < n * L; i += 256) {
+    for (int i = threadIdx.x; i < n * L; i += NT) {
       const int r = r0 + i / L, ch = i % L, nr = a.by_group.quot(r);
       Row16<BF16> x;
       x.load((const char*)a.q +
@@ -476,8 +470,24 @@ __global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int j = j0 + u * PP + threadIdx.x / L;
-    if (c == 0 && j < pages) a.score[(long long)bh * p.max_pages + j] = nan[u] ? (double)NAN : best[u];
+    if (c == 0 && j < pages) put(j, nan[u] ? (double)NAN : best[u]);
   }
+}
+
+template <bool BF16, int D>
+__global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
+  constexpr int PP = 256 / (D / (BF16 ? 8 : 4));
+  __shared__ __align__(16) float q[16][D];
+  const PagedArgs& p = a.c;
+  const int id = uniform((int)block_id());
+  const int bh = a.by_blocks.quot(id);
+  const int b = a.by_heads.quot(bh), g = a.by_heads.rem(bh, b);
+  if (b >= p.B) return;
+  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
+  const int j0 = a.by_blocks.rem(id, bh) * PP * kScoreTurns;
+  if (j0 >= pages) return;
+  double* score = a.score + (long long)bh * p.max_pages;
+  score_pages<BF16, D, 256>(a, b, g, j0, pages, paged_new(p, b) * p.G, q, [&](int j, double s) { score[j] = s; });
 }
 
 // The top_k pages of one (sequence, KV head), ascending.  Scores map to 64-bit keys whose
@@ -508,16 +518,11 @@ __device__ __forceinline__ int block_prefix(int x, int* lds) {
 }
 
 template <int KPT>
-__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectArgs a) {
+__device__ __forceinline__ void select_pages(const PageSelectArgs& a, const double* score, int pages, int32_t* out) {
   __shared__ uint32_t hist[256];
   __shared__ uint64_t all_or[kSelectWaves], all_and[kSelectWaves];
   __shared__ int sums[2][kSelectWaves], pick[3];
-  const PagedArgs& p = a.c;
-  const int bh = uniform((int)block_id()), b = a.by_heads.quot(bh), tid = threadIdx.x;
-  if (b >= p.B) return;
-  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
-  const double* score = a.score + (long long)bh * p.max_pages;
-  int32_t* out = a.page_idx + (long long)bh * a.top_k;
+  const int tid = threadIdx.x;
   const int k = min(a.top_k, pages);
   for (int i = k + tid; i < a.top_k; i += kSelectThreads) out[i] = -1;
   // Forced pages: 0..head-1 and tail..pages-1.
@@ -618,6 +623,40 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectA
   }
 }
 
+template <int KPT>
+__global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectArgs a) {
+  const PagedArgs& p = a.c;
+  const int bh = uniform((int)block_id()), b = a.by_heads.quot(bh);
+  if (b >= p.B) return;
+  select_pages<KPT>(a, a.score + (long long)bh * p.max_pages, (paged_len(p, b) + p.R - 1) >> p.log2R,
+                    a.page_idx + (long long)bh * a.top_k);
+}
+
+// Scores and choice in one launch, a workgroup for each (sequence, KV head), the scores in LDS.
+constexpr int kFusedPages = 512;
+template <bool BF16, int D>
+__global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(PageSelectArgs a) {
+  constexpr int PP = kSelectThreads / (D / (BF16 ? 8 : 4));
+  __shared__ __align__(16) float q[16][D];
+  __shared__ double score[kFusedPages];
+  const PagedArgs& p = a.c;
+  const int bh = uniform((int)block_id());
+  const int b = a.by_heads.quot(bh), g = a.by_heads.rem(bh, b);
+  if (b >= p.B) return;
+  const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R, rows = paged_new(p, b) * p.G;
+  if (pages > a.top_k)   // otherwise all are kept
+    for (int j0 = 0; j0 < pages; j0 += PP * kScoreTurns)
+      score_pages<BF16, D, kSelectThreads>(a, b, g, j0, pages, rows, q, [&](int j, double s) { score[j] = s; });
+  __syncthreads();
+  select_pages<1>(a, score, pages, a.page_idx + (long long)bh * a.top_k);
+}
+
+// Whether one launch does: the pages of a (sequence, head) are few, or there is such a
+// workgroup for every CU (FILL_IN).
+bool page_select_fused(const PagedArgs& p) {
+  return p.max_pages <= 128 || (p.max_pages <= kFusedPages && (long long)p.B * p.Hkv >= kNumCu);
+}
+
 int page_score_blocks(const PagedArgs& p) {
   const int per = 256 / (p.D / (p.bf16 ? 8 : 4)) * kScoreTurns;
   return (p.max_pages + per - 1) / per;
@@ -625,6 +664,17 @@ int page_score_blocks(const PagedArgs& p) {
 
 hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s) {
   const PagedArgs& p = a.c;
+  const dim3 sg = grid_xy((long long)p.B * p.Hkv);
+  if (page_select_fused(p)) {
+    if (p.bf16) {
+      if (p.D == 128) hipLaunchKernelGGL((page_score_select_kernel<true, 128>), sg, dim3(kSelectThreads), 0, s, a);
+      else hipLaunchKernelGGL((page_score_select_kernel<true, 64>), sg, dim3(kSelectThreads), 0, s, a);
+    } else {
+      if (p.D == 128) hipLaunchKernelGGL((page_score_select_kernel<false, 128>), sg, dim3(kSelectThreads), 0, s, a);
+      else hipLaunchKernelGGL((page_score_select_kernel<false, 64>), sg, dim3(kSelectThreads), 0, s, a);
+    }
+    return hipGetLastError();
+  }
   const dim3 grid = grid_xy((long long)p.B * p.Hkv * page_score_blocks(p));
   if (p.bf16) {
     if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<true, 128>), grid, dim3(256), 0, s, a);
@@ -635,7 +685,6 @@ hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 sg = grid_xy((long long)p.B * p.Hkv);
   if (p.max_pages <= kSelectThreads) hipLaunchKernelGGL(page_select_kernel<1>, sg, dim3(kSelectThreads), 0, s, a);
   else if (p.max_pages <= 4 * kSelectThreads) hipLaunchKernelGGL(page_select_kernel<4>, sg, dim3(kSelectThreads), 0, s, a);
   else if (p.max_pages <= 16 * kSelectThreads) hipLaunchKernelGGL(page_select_kernel<16>, sg, dim3(kSelectThreads), 0, s, a);

@@ -182,13 +182,21 @@ struct PagedStep {
   int pos[S::H];                 // position of the first key of each 16
 };
 
+// Over the four lanes n, 16 + n, 32 + n, 48 + n of a query row: halves, then neighbouring rows
+// of 16 lanes, exchanged on the vector units.
+template <class F>
+__device__ __forceinline__ float over_groups(float x, F op) {
+  const uint32_t u = __float_as_uint(x);
+  const auto h = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const uint32_t w = __float_as_uint(op(__uint_as_float(h[0]), __uint_as_float(h[1])));
+  const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 __device__ __forceinline__ float group_max(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  return over_groups(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float group_sum(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  return over_groups(x, [](float a, float b) { return a + b; });
 }
 
 template <bool STREAM, class T>
@@ -202,7 +210,7 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 // STREAM: the keys are read by one workgroup alone (non-temporal loads: 8 x 32K keys 654
 // against 718 us); row blocks that share them leave them in the caches.
 template <int D, int CT, int RT, bool STREAM>
-__global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, RT == 1 || D == 64 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
@@ -350,9 +358,8 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
     }
     // A key that some rows see and others do not: its value has to stay out of the others
     // even where it is not finite, which a weight of zero does not achieve.  Such values are
-    // taken out of the products and go in by themselves: which of the lane's are +inf, -inf
-    // and NaN, a bit each.
-    uint64_t odd[3] = {0, 0, 0};
+    // zeros in the products, and are added by themselves to the rows that see them, from a
+    // copy of the step's values in the wave's part of lds_o.
     bool any_odd = false;
     if (!whole && p.causal && n_new > 1) {
       float z = 0.f;
@@ -369,24 +376,22 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         }
       any_odd = __any(z != z);
       if (any_odd) {
-        auto sort_out = [&](float x, int at) {
-          if (x == INFINITY) odd[0] |= 1ull << at;
-          if (x == -INFINITY) odd[1] |= 1ull << at;
-          if (x != x) odd[2] |= 1ull << at;
-          return fabsf(x) < INFINITY;
-        };
+        uint32_t* copy = (uint32_t*)&lds_o[wave][0][0];   // [key of the step][channels]
 #pragma unroll
         for (int j = 0; j < VR; ++j)
 #pragma unroll
           for (int w = 0; w < W; ++w) {
+            const int key = 16 * (j / 4) + 4 * g4 + j % 4;
+            const int at = CT == kFp32 ? 64 * (w / 4) + 4 * n + w % 4 : (E * n + 2 * w) / 2;
+            copy[key * (CT == kFp32 ? D : D / 2) + at] = v[j][w];
             if constexpr (CT == kFp32) {
-              if (!sort_out(__uint_as_float(v[j][w]), j * W + w)) v[j][w] = 0u;
+              if (!(fabsf(__uint_as_float(v[j][w])) < INFINITY)) v[j][w] = 0u;
             } else {
-              const bool lo = sort_out(__uint_as_float(v[j][w] << 16), (j * W + w) * 2);
-              const bool hi = sort_out(__uint_as_float(v[j][w] & 0xffff0000u), (j * W + w) * 2 + 1);
-              v[j][w] &= (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
+              if ((v[j][w] & 0x7f80u) == 0x7f80u) v[j][w] &= 0xffff0000u;
+              if ((v[j][w] & 0x7f800000u) == 0x7f800000u) v[j][w] &= 0xffffu;
             }
           }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
     }
 #pragma unroll
@@ -473,79 +478,60 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
         }
       }
       if (!whole && any_odd) {
-        // How many values of each kind a row sees in a channel, as a product of zeros and ones.
-        float one[H][4];
+        for (int key = 0; key < S::KS; ++key) {
+          if ((key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16 >= lim[t]) continue;
+          const float* copy = &lds_o[wave][0][0] + key * (CT == kFp32 ? D : D / 2);
 #pragma unroll
-        for (int h = 0; h < H; ++h)
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) one[h][e] = s.pos[h] + 4 * g4 + e < lim[t] ? 1.f : 0.f;
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-          for (int kind = 0; kind < 3; ++kind) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f};
-            if constexpr (CT == kFp32) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j)
-                x = __builtin_amdgcn_mfma_f32_16x16x4f32((odd[kind] >> (j * W + i)) & 1 ? 1.f : 0.f, one[0][j], x, 0, 0, 0);
-            } else {
-              u32x4 w, pw;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                w[j] = ((odd[kind] >> (4 * j * W + i)) & 1 ? 0x3f80u : 0u) |
-                       ((odd[kind] >> ((4 * j + 2) * W + i)) & 1 ? 0x3f800000u : 0u);
-                pw[j] = pack_bf16x2(one[j / 2][2 * (j & 1)], one[j / 2][2 * (j & 1) + 1]);
-              }
-              x = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), x);
+            for (int i = 0; i < NT; ++i) {
+              const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : E * (4 * g4 + r) + i;
+              const uint32_t u = __float_as_uint(copy[CT == kFp32 ? ch : ch / 2]);
+              const float x = __uint_as_float(CT == kFp32 ? u : i & 1 ? u & 0xffff0000u : u << 16);
+              if (!(fabsf(x) < INFINITY)) o[t][i][r] += x;
             }
-            const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (x[e] != 0.f) o[t][i][e] += add;
-          }
+        }
       }
     }
   };
 
-  // Whole steps first, the next one's loads in flight; from the first other one on (the end
-  // of the rows, the new rows' own positions) step by step, with masks.
-  auto whole_at = [&](int i) {
-    bool w = true;
-#pragma unroll
-    for (int h = 0; h < H; ++h) w = w && __builtin_amdgcn_readlane(at_pos[h], i & 63) + 16 <= every;
-    return w;
-  };
+  // Whole steps first, each with the loads of the next one in flight (there is one: the wait for
+  // a step's own loads can only be counted past the next one's where those are always
+  // issued).  From the first other step on (the last one, the end of the rows, the new rows'
+  // own positions) step by step, with masks.
   if (n_steps > 0) {
     PagedStep<D, CT> s0, s1;
     int i = 0;
-    auto next = [&](PagedStep<D, CT>& s) {   // step i + 1, if there is one; whether it is whole
-      if (i + 1 >= n_steps) return false;
+    auto whole_before_another = [&]() {
+      bool w = i + 1 < n_steps;
+#pragma unroll
+      for (int h = 0; h < H; ++h) w = w && __builtin_amdgcn_readlane(at_pos[h], i & 63) + 16 <= every;
+      return w;
+    };
+    auto fetch_next = [&](PagedStep<D, CT>& s) {
       if (((i + 1) & 63) == 0) locate(i + 1);
       load(s, i + 1);
       __builtin_amdgcn_sched_barrier(0);
-      return whole_at(i + 1);
     };
     locate(0);
     load(s0, 0);
-    bool whole = whole_at(0);
-    while (whole) {
-      whole = next(s1);
+    while (whole_before_another()) {
+      fetch_next(s1);
       compute(s0, std::true_type{});
       ++i;
-      if (!whole) {
+      if (!whole_before_another()) {
         s0 = s1;
         break;
       }
-      whole = next(s0);
+      fetch_next(s0);
       compute(s1, std::true_type{});
       ++i;
     }
-    while (i < n_steps) {
+    for (;;) {
       compute(s0, std::false_type{});
-      if (++i < n_steps) {
-        if ((i & 63) == 0) locate(i);
-        load(s0, i);
-      }
+      if (++i >= n_steps) break;
+      if ((i & 63) == 0) locate(i);
+      load(s0, i);
     }
   }
 
@@ -621,26 +607,36 @@ __global__ __launch_bounds__(256, RT == 1 ? 2 : 1) void paged_attn_kernel(PagedA
 }
 
 // The join of rows whose keys were cut: o = sum_s 2^(m_s - M) O_s / sum_s 2^(m_s - M) l_s in the
-// parts' order.  One workgroup a row; its threads take four channels of every
-// (1024 / D)-th part each, all loads of eight parts in flight, and are joined through LDS.
-template <int D, bool BF16>
+// parts' order.  A thread takes four channels of every SL-th part, with the loads of eight
+// parts in flight, and the slices are joined through LDS.  RW rows a workgroup: one where
+// there are few rows, which may have many parts each; four where there are many rows and
+// so few parts (rows of one part only end sooner then: 13 x 16 heads x 33 rows 3.0 us, one a
+// workgroup 5.6).
+template <int D, bool BF16, int RW>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
-  constexpr int T = D / 4, SL = 256 / T, U = 8;   // threads of a row, slices of the parts
-  __shared__ f32x4 lds_o[SL][T];
-  __shared__ float lds_m[SL], lds_l[SL];
+  constexpr int T = D / 4, SL = 256 / T / RW, U = 8;   // threads of a row, slices of the parts
+  __shared__ f32x4 lds_o[RW][SL][T];
+  __shared__ float lds_m[RW][SL], lds_l[RW][SL];
   const PagedArgs& p = a.c;
-  const int id = uniform((int)block_id());
+  const int rw = threadIdx.x / (T * SL), c = threadIdx.x % T, sl = threadIdx.x / T % SL;
+  const int id = uniform((int)block_id()) * RW + rw;
   const int bg = a.by_rows.quot(id), r = a.by_rows.rem(id, bg);
   const int b = a.by_heads.quot(bg), g = a.by_heads.rem(bg, b);
-  if (b >= p.B) return;
   const int rb = r / kPagedRows, rl = r - rb * kPagedRows;
-  const int32_t* unit = a.unit + ((long long)bg * a.row_blocks + rb) * 4;
-  const int first = unit[0], parts = unit[1];
-  if (parts == 1 || rl >= unit[2]) return;
-  const int c = threadIdx.x % T, sl = threadIdx.x / T;
+  int first = 0, parts = 1, rows = 0;
+  if (b < p.B) {
+    const int32_t* unit = a.unit + ((long long)bg * a.row_blocks + rb) * 4;
+    first = unit[0];
+    parts = unit[1];
+    rows = unit[2];
+  }
+  const bool live = parts > 1 && rl < rows;
+  if constexpr (RW == 1) {
+    if (!live) return;
+  }
   float M = kNoMax, L = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int s0 = sl; s0 < parts; s0 += SL * U) {
+  for (int s0 = sl; live && s0 < parts; s0 += SL * U) {
     float ms[U], ls[U];
     f32x4 v[U];
 #pragma unroll
@@ -665,22 +661,22 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
         acc += w * v[u];
       }
   }
-  lds_o[sl][c] = acc;
+  lds_o[rw][sl][c] = acc;
   if (c == 0) {
-    lds_m[sl] = M;
-    lds_l[sl] = L;
+    lds_m[rw][sl] = M;
+    lds_l[rw][sl] = L;
   }
   __syncthreads();
-  if (sl > 0) return;
+  if (sl > 0 || !live) return;
 #pragma unroll
-  for (int s = 0; s < SL; ++s) M = fmaxf(M, lds_m[s]);
+  for (int s = 0; s < SL; ++s) M = fmaxf(M, lds_m[rw][s]);
   L = 0.f;
   acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < SL; ++s) {
-    const float w = fast_exp2(lds_m[s] - M);
-    L += w * lds_l[s];
-    acc += w * lds_o[s][c];
+    const float w = fast_exp2(lds_m[rw][s] - M);
+    L += w * lds_l[rw][s];
+    acc += w * lds_o[rw][s][c];
   }
   const int nr = a.by_group.quot(r), head = g * p.G + a.by_group.rem(r, nr);
   const long long el = (((long long)b * p.Ln + nr) * p.Hq + head) * D + 4 * c;
@@ -701,8 +697,9 @@ hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, false>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_chunks == 1) return e;
-  hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32>),
-                     grid_xy((long long)a.c.B * a.c.Hkv * rows), dim3(256), 0, s, a);
+  const long long all = (long long)a.c.B * a.c.Hkv * rows;
+  if (all >= 4 * kNumCu) hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32, 4>), grid_xy((all + 3) / 4), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_join_kernel<D, CT != kFp32, 1>), grid_xy(all), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
