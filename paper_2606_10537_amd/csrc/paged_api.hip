@@ -111,7 +111,7 @@ long long touched_pages(const pd_paged_dims* d) {
 
 // --- attention: how the keys are cut, and the workspace of the parts -----------
 struct AttnPlan {
-  int row_blocks, part_rows, max_chunks;
+  int row_blocks, part_rows, parts, max_chunks;
   long long grid;
   size_t o_bytes, ml_bytes, total;
 };
@@ -125,10 +125,11 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   if (units >= kMaxGrid / 2 || (double)units * (double)blocks >= 9e18)
     return fail(PD_ERR_BAD_DIMS, "attention of batch=%d with new_len=%d is too large for one launch", d->batch,
                 d->new_len);
-  p->max_chunks = (int)std::min<long long>(blocks, pd::kPagedParts);
-  // The kernels cut with a quota of at least all blocks / kPagedParts: at most so many
-  // whole quotas, and one part that is not whole for each unit.
-  p->grid = p->max_chunks == 1 ? units : std::min(units + pd::kPagedParts, units * p->max_chunks);
+  p->parts = pd::paged_parts(rows);
+  p->max_chunks = (int)std::min<long long>(blocks, p->parts);
+  // The kernels cut with a quota of at least all blocks / parts: at most so many whole
+  // quotas, and one part that is not whole for each unit.
+  p->grid = p->max_chunks == 1 ? units : std::min(units + p->parts, units * p->max_chunks);
   const size_t slots = p->max_chunks == 1 ? 0 : (size_t)p->grid * p->part_rows;
   p->o_bytes = round_up(slots * d->head_dim * sizeof(float));
   p->ml_bytes = round_up(slots * 2 * sizeof(float));
@@ -314,6 +315,7 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.row_blocks = plan.row_blocks;
   a.part_rows = plan.part_rows;
   a.max_chunks = plan.max_chunks;
+  a.per_part = 1.0f / plan.parts;
   a.grid = plan.grid;
   a.by_group = pd::fast_div(a.c.G);
   a.by_heads = pd::fast_div(a.c.Hkv);

@@ -50,7 +50,7 @@ struct PagedPart {
 //
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
 // card at once are cut into as few parts as give every CU one.  Otherwise parts of 16 blocks
-// or more, 2048 of them where the keys suffice, so that the workgroups of short
+// or more, paged_parts of them where the keys suffice, so that the workgroups of short
 // sequences and the ends of long ones fill in.  Measured, 2 CU-filling parts against 8: 8 x 32
 // heads x 8K keys 170 against 179 us, 8 x 8 heads x 32K 175 against 188, 64 ragged
 // sequences in 8 bits 474 against 382 us.
@@ -76,7 +76,7 @@ __device__ __forceinline__ int short_div(int n, int d) {
   q += r >= d ? 1 : 0;
   return r < 0 ? q - 1 : q;
 }
-// ceil(blocks / quota), at most kPagedParts + 1.
+// ceil(blocks / quota), at most paged_parts + 1.
 __device__ __forceinline__ int parts_of(int blocks, int quota) {
   return blocks <= quota ? 1 : short_div(blocks - 1, quota) + 1;
 }
@@ -89,6 +89,7 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   auto larger = [](int x, int y) { return max(x, y); };
   const PagedSeq head = paged_seq<BK>(a, lane);
   int quota = 1 << 30;
+  bool even = true;
   if (a.max_chunks > 1) {
     // In fp32, which a quota need not be exact for: an error of 2^-12 in it still leaves the
     // number of parts below what the host has made room for.
@@ -105,15 +106,41 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       const int c = (int)fminf(x, 1073741824.f);
       return (float)c < x ? c + 1 : c;
     };
-    const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * (1.f / kPagedParts));
-    const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
+    const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
+    even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
     quota = max(1, uniform(even ? fill : max(fine, min(fill, 16))));
   }
+  // Order: the parts of a whole quota, then the shorter ends, which even out when the
+  // workgroups finish.  `whole` of a sequence's `parts` come in the first turn.
+  struct Cut {
+    int parts, whole;
+  };
+  auto cut = [&](int b, const PagedSeq& s) {
+    Cut c{0, 0};
+    if (b < p.B) {
+      c.parts = parts_of(s.blocks, quota);
+      c.whole = even || c.parts * quota == s.blocks ? c.parts : c.parts - 1;
+    }
+    return c;
+  };
+  int first_turn = 0x7fffffff;
+  if (!even) {
+    first_turn = 0;
+    for (int b0 = 0; b0 < p.B; b0 += 64)
+      first_turn += __builtin_amdgcn_readlane(
+          wave_scan(cut(b0 + lane, b0 == 0 ? head : paged_seq<BK>(a, b0 + lane)).whole, 0, add), 63);
+    first_turn *= units;
+  }
+  const bool second = find >= first_turn;
+  if (second) find -= first_turn;
   PagedPart r{};
-  int before = 0;
+  int before = 0, before_all = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const PagedSeq s = b0 == 0 ? head : paged_seq<BK>(a, b0 + lane);
-    const int incl = before + wave_scan(b0 + lane < p.B ? parts_of(s.blocks, quota) * units : 0, 0, add);
+    const Cut c = cut(b0 + lane, s);
+    const int own = (second ? c.parts - c.whole : c.whole) * units;
+    const int incl = before + wave_scan(own, 0, add);
+    const int incl_all = even ? incl : before_all + wave_scan(c.parts * units, 0, add);
     const uint64_t past = __ballot(incl > find);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
@@ -121,15 +148,16 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       r.b = b0 + l;
       r.len = __builtin_amdgcn_readlane(s.len, l);
       r.n_new = __builtin_amdgcn_readlane(s.n_new, l);
-      r.parts = parts_of(n, quota);
-      const int base = __builtin_amdgcn_readlane(incl, l) - r.parts * units;
+      r.parts = __builtin_amdgcn_readlane(c.parts, l);
+      const int mine = __builtin_amdgcn_readlane(own, l);
+      const int each = second ? 1 : __builtin_amdgcn_readlane(c.whole, l);   // of a unit in this turn
       // Row blocks of the same keys run on one XCD, eight workgroups apart, so that all but
       // the first find them in its L2.
-      const int i = find - base;
+      const int i = find - (__builtin_amdgcn_readlane(incl, l) - mine);
       int pair = i;
       r.rb = 0;
       if (a.row_blocks > 1) {
-        if (i < p.Hkv * r.parts / kNumXcd * kNumXcd * a.row_blocks) {
+        if (i < p.Hkv * each / kNumXcd * kNumXcd * a.row_blocks) {
           const int q = a.by_blocks.quot(i / kNumXcd);
           r.rb = a.by_blocks.rem(i / kNumXcd, q);
           pair = q * kNumXcd + i % kNumXcd;
@@ -138,21 +166,20 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
           r.rb = a.by_blocks.rem(i, pair);
         }
       }
-      r.slot = base + pair * a.row_blocks + r.rb;
-      r.index = 0;
       r.g = pair;
-      r.first = 0;
-      r.last = n;
-      if (r.parts > 1) {
-        r.g = short_div(pair, r.parts);
-        r.index = pair - r.g * r.parts;
-        r.first = r.index * quota;
-        r.last = min(r.first + quota, n);
+      r.index = second ? r.parts - 1 : 0;
+      if (each > 1) {
+        r.g = short_div(pair, each);
+        r.index = pair - r.g * each;
       }
+      r.first = r.parts > 1 ? r.index * quota : 0;
+      r.last = r.parts > 1 ? min(r.first + quota, n) : n;
+      r.slot = __builtin_amdgcn_readlane(incl_all, l) - r.parts * units + (r.g * r.parts + r.index) * a.row_blocks + r.rb;
       r.any = true;
       return r;
     }
     before = __builtin_amdgcn_readlane(incl, 63);
+    before_all = __builtin_amdgcn_readlane(incl_all, 63);
   }
   return r;
 }

@@ -91,11 +91,16 @@ struct PagedAttnArgs {
   int32_t* unit;         // [B][H_kv][row_blocks][4]: a unit's first part, parts and rows
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
+  float per_part;        // 1 / paged_parts
   long long grid;
   FastDiv by_group, by_heads, by_rows, by_blocks;  // G, H_kv, G * L_n, row_blocks
 };
-// Parts that the keys of a ragged batch are cut into at most, besides one for every unit.
-constexpr int kPagedParts = 2048;
+// Parts that the keys of a ragged batch are cut into at most, besides one for every unit, for
+// `rows` query rows of a KV head.  How many there are is known on the device alone, so as many
+// workgroups are launched, and one that finds no part costs its launch: little where a CU
+// holds two or more, but 4 us for a thousand of those with more than 16 rows, of which it holds
+// one (8 rows of 4 heads over 8 x 8K keys 53.5 us with 2048, 57.5 with 3072).
+inline int paged_parts(long long rows) { return rows <= 16 ? 3072 : 1024; }
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
