@@ -505,6 +505,14 @@ __device__ __forceinline__ uint64_t page_key(double s) {
   return (u >> 63) ? ~u : (u | (1ull << 63));
 }
 
+// Bitwise reduction over the wave.
+template <class F>
+__device__ __forceinline__ uint64_t wave_bits(uint64_t x, int none, F op) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)(uint32_t)x, none, op), 63);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane(wave_scan((int)(uint32_t)(x >> 32), none, op), 63);
+  return (uint64_t)hi << 32 | lo;
+}
+
 // Exclusive sum over the workgroup of one value per thread.
 __device__ __forceinline__ int block_prefix(int x, int* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -552,11 +560,8 @@ __device__ __forceinline__ void select_pages(const PageSelectArgs& a, const doub
     any |= x;
     every &= x;
   });
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    any |= __shfl_xor(any, m);
-    every &= __shfl_xor(every, m);
-  }
+  any = wave_bits(any, 0, [](int x, int y) { return x | y; });
+  every = wave_bits(every, -1, [](int x, int y) { return x & y; });
   if ((tid & 63) == 0) {
     all_or[tid >> 6] = any;
     all_and[tid >> 6] = every;
@@ -633,7 +638,7 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectA
 }
 
 // Scores and choice in one launch, a workgroup for each (sequence, KV head), the scores in LDS.
-constexpr int kFusedPages = 512;
+constexpr int kFusedPages = 128;
 template <bool BF16, int D>
 __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(PageSelectArgs a) {
   constexpr int PP = kSelectThreads / (D / (BF16 ? 8 : 4));
@@ -651,11 +656,10 @@ __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(PageS
   select_pages<1>(a, score, pages, a.page_idx + (long long)bh * a.top_k);
 }
 
-// Whether one launch does: the pages of a (sequence, head) are few, or there is such a
-// workgroup for every CU (FILL_IN).
-bool page_select_fused(const PagedArgs& p) {
-  return p.max_pages <= 128 || (p.max_pages <= kFusedPages && (long long)p.B * p.Hkv >= kNumCu);
-}
+// Whether one launch does: few pages (128 pages of 8 heads 17.2 us with the attention over 16 of
+// them, 17.7 with two launches).  More are scored by more workgroups (512 pages of 8 x 32 heads
+// 46.4 us in one launch, 45.4 in two).
+bool page_select_fused(const PagedArgs& p) { return p.max_pages <= kFusedPages; }
 
 int page_score_blocks(const PagedArgs& p) {
   const int per = 256 / (p.D / (p.bf16 ? 8 : 4)) * kScoreTurns;
