@@ -416,11 +416,13 @@ __device__ __forceinline__ double lanes_sum(double x) {
 }
 
 constexpr int kScoreTurns = 4;   // pages of a lane
-// Scores of pages j0 .. of (b, g), four pages a lane of NT threads; put(j, score).
+constexpr int kScoreRows = 16;   // query rows in LDS at a time
+// Scores of pages j0 .. of (b, g) over the query rows of every step-th block from block r0 on, four
+// pages a lane of NT threads; put(j, score).
 template <bool BF16, int D, int NT, class F>
 __device__ __forceinline__ void score_pages(const PageSelectArgs& a, int b, int g, int j0, int pages, int rows,
-                                            float (&q)[16][D], F put) {
-  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = NT / L, EB = BF16 ? 2 : 4, QR = 16, U = kScoreTurns;
+                                            int block0, int step, float (&q)[kScoreRows][D], F put) {
+  constexpr int E = BF16 ? 8 : 4, L = D / E, PP = NT / L, EB = BF16 ? 2 : 4, QR = kScoreRows, U = kScoreTurns;
   const PagedArgs& p = a.c;
   const int c = threadIdx.x % L;
   Row16<BF16> lo[U], hi[U];
@@ -438,7 +440,7 @@ __device__ __forceinline__ void score_pages(const PageSelectArgs& a, int b, int 
   double best[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) best[u] = -INFINITY;
-  for (int r0 = 0; r0 < rows; r0 += QR) {
+  for (int r0 = block0 * QR; r0 < rows; r0 += step * QR) {
     const int n = min(QR, rows - r0);
     __syncthreads();
     for (int i = threadIdx.x; i < n * L; i += NT) {
@@ -455,6 +457,7 @@ __device__ __forceinline__ void score_pages(const PageSelectArgs& a, int b, int 
       for (int e = 0; e < E; ++e) x[e] = q[r][c * E + e];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (u > 0 && j0 + u * PP >= pages) break;   // no pages in this turn
         float l32[E], h32[E];
         lo[u].unpack(l32);
         hi[u].unpack(h32);
@@ -477,17 +480,18 @@ __device__ __forceinline__ void score_pages(const PageSelectArgs& a, int b, int 
 template <bool BF16, int D>
 __global__ __launch_bounds__(256) void page_score_kernel(PageSelectArgs a) {
   constexpr int PP = 256 / (D / (BF16 ? 8 : 4));
-  __shared__ __align__(16) float q[16][D];
+  __shared__ __align__(16) float q[kScoreRows][D];
   const PagedArgs& p = a.c;
   const int id = uniform((int)block_id());
-  const int bh = a.by_blocks.quot(id);
+  const int all = a.by_blocks.quot(id), bh = a.by_shares.quot(all), share = a.by_shares.rem(all, bh);
   const int b = a.by_heads.quot(bh), g = a.by_heads.rem(bh, b);
   if (b >= p.B) return;
   const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R;
-  const int j0 = a.by_blocks.rem(id, bh) * PP * kScoreTurns;
+  const int j0 = a.by_blocks.rem(id, all) * PP * kScoreTurns;
   if (j0 >= pages) return;
-  double* score = a.score + (long long)bh * p.max_pages;
-  score_pages<BF16, D, 256>(a, b, g, j0, pages, paged_new(p, b) * p.G, q, [&](int j, double s) { score[j] = s; });
+  double* score = a.score + (long long)all * p.max_pages;
+  score_pages<BF16, D, 256>(a, b, g, j0, pages, paged_new(p, b) * p.G, share, a.shares, q,
+                            [&](int j, double s) { score[j] = s; });
 }
 
 // The top_k pages of one (sequence, KV head), ascending.  Scores map to 64-bit keys whose
@@ -525,8 +529,10 @@ __device__ __forceinline__ int block_prefix(int x, int* lds) {
   return before + incl - x;
 }
 
+// score: of page j of row share i at i * stride + j.
 template <int KPT>
-__device__ __forceinline__ void select_pages(const PageSelectArgs& a, const double* score, int pages, int32_t* out) {
+__device__ __forceinline__ void select_pages(const PageSelectArgs& a, const double* score, int shares, int stride,
+                                             int pages, int32_t* out) {
   __shared__ uint32_t hist[256];
   __shared__ uint64_t all_or[kSelectWaves], all_and[kSelectWaves];
   __shared__ int sums[2][kSelectWaves], pick[3];
@@ -541,9 +547,14 @@ __device__ __forceinline__ void select_pages(const PageSelectArgs& a, const doub
   }
   int need = k - forced;                // pages still to be taken among those that match the prefix
   const int per = (pages + kSelectThreads - 1) / kSelectThreads, j0 = tid * per;
+  auto key_of = [&](int j) {            // NaN ranks first, so the largest key is the largest score's
+    uint64_t x = page_key(score[j]);
+    for (int i = 1; i < shares; ++i) x = max(x, page_key(score[(long long)i * stride + j]));
+    return x;
+  };
   uint64_t key[KPT > 0 ? KPT : 1];
 #pragma unroll
-  for (int t = 0; t < KPT; ++t) key[t] = t < per && j0 + t < pages ? page_key(score[j0 + t]) : 0;
+  for (int t = 0; t < KPT; ++t) key[t] = t < per && j0 + t < pages ? key_of(j0 + t) : 0;
   auto free_page = [&](int j) { return j >= head && j < tail; };
   auto each = [&](auto f) {             // f(page, key) for the thread's pages that are not forced
     if constexpr (KPT > 0) {
@@ -552,7 +563,7 @@ __device__ __forceinline__ void select_pages(const PageSelectArgs& a, const doub
         if (t < per && free_page(j0 + t)) f(j0 + t, key[t]);
     } else {
       for (int t = 0; t < per; ++t)
-        if (free_page(j0 + t)) f(j0 + t, page_key(score[j0 + t]));
+        if (free_page(j0 + t)) f(j0 + t, key_of(j0 + t));
     }
   };
   uint64_t any = 0, every = ~0ull;
@@ -633,8 +644,8 @@ __global__ __launch_bounds__(kSelectThreads) void page_select_kernel(PageSelectA
   const PagedArgs& p = a.c;
   const int bh = uniform((int)block_id()), b = a.by_heads.quot(bh);
   if (b >= p.B) return;
-  select_pages<KPT>(a, a.score + (long long)bh * p.max_pages, (paged_len(p, b) + p.R - 1) >> p.log2R,
-                    a.page_idx + (long long)bh * a.top_k);
+  select_pages<KPT>(a, a.score + (long long)bh * a.shares * p.max_pages, a.shares, p.max_pages,
+                    (paged_len(p, b) + p.R - 1) >> p.log2R, a.page_idx + (long long)bh * a.top_k);
 }
 
 // Scores and choice in one launch, a workgroup for each (sequence, KV head), the scores in LDS.
@@ -642,7 +653,7 @@ constexpr int kFusedPages = 128;
 template <bool BF16, int D>
 __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(PageSelectArgs a) {
   constexpr int PP = kSelectThreads / (D / (BF16 ? 8 : 4));
-  __shared__ __align__(16) float q[16][D];
+  __shared__ __align__(16) float q[kScoreRows][D];
   __shared__ double score[kFusedPages];
   const PagedArgs& p = a.c;
   const int bh = uniform((int)block_id());
@@ -651,15 +662,23 @@ __global__ __launch_bounds__(kSelectThreads) void page_score_select_kernel(PageS
   const int pages = (paged_len(p, b) + p.R - 1) >> p.log2R, rows = paged_new(p, b) * p.G;
   if (pages > a.top_k)   // otherwise all are kept
     for (int j0 = 0; j0 < pages; j0 += PP * kScoreTurns)
-      score_pages<BF16, D, kSelectThreads>(a, b, g, j0, pages, rows, q, [&](int j, double s) { score[j] = s; });
+      score_pages<BF16, D, kSelectThreads>(a, b, g, j0, pages, rows, 0, 1, q, [&](int j, double s) { score[j] = s; });
   __syncthreads();
-  select_pages<1>(a, score, pages, a.page_idx + (long long)bh * a.top_k);
+  select_pages<1>(a, score, 1, 0, pages, a.page_idx + (long long)bh * a.top_k);
 }
 
 // Whether one launch does: few pages (128 pages of 8 heads 17.2 us with the attention over 16 of
 // them, 17.7 with two launches).  More are scored by more workgroups (512 pages of 8 x 32 heads
 // 46.4 us in one launch, 45.4 in two).
-bool page_select_fused(const PagedArgs& p) { return p.max_pages <= kFusedPages; }
+bool page_select_fused(const PagedArgs& p) { return p.max_pages <= kFusedPages && p.G * p.Ln <= kScoreRows; }
+
+// Shares that the query rows of a (sequence, head) are scored in, each by workgroups of its own: the
+// blocks of 16 rows, at most eight shares (264 rows over 17 pages of 13 heads, and the attention over 6 of
+// them: 223 us with one share, 35 with eight).
+int page_score_shares(const PagedArgs& p) {
+  const long long blocks = ((long long)p.G * p.Ln + kScoreRows - 1) / kScoreRows;
+  return (int)(blocks < 8 ? blocks : 8);
+}
 
 int page_score_blocks(const PagedArgs& p) {
   const int per = 256 / (p.D / (p.bf16 ? 8 : 4)) * kScoreTurns;
@@ -679,7 +698,7 @@ hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s) {
     }
     return hipGetLastError();
   }
-  const dim3 grid = grid_xy((long long)p.B * p.Hkv * page_score_blocks(p));
+  const dim3 grid = grid_xy((long long)p.B * p.Hkv * a.shares * page_score_blocks(p));
   if (p.bf16) {
     if (p.D == 128) hipLaunchKernelGGL((page_score_kernel<true, 128>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((page_score_kernel<true, 64>), grid, dim3(256), 0, s, a);

@@ -137,8 +137,15 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   return PD_OK;
 }
 
+// What the kernels go by of the sizes alone.
+pd::PagedArgs sizes_of(const pd_paged_dims* d) {
+  const pd_paged_cache none{};
+  return paged_args(d, &none);
+}
+
 size_t select_bytes(const pd_paged_dims* d) {
-  return round_up((size_t)d->batch * d->n_heads_kv * d->max_pages * sizeof(double));
+  const int shares = pd::page_score_shares(sizes_of(d));
+  return round_up((size_t)d->batch * d->n_heads_kv * shares * d->max_pages * sizeof(double));
 }
 
 pd_status check_select_dims(const pd_paged_dims* d, int top_k) {
@@ -146,8 +153,9 @@ pd_status check_select_dims(const pd_paged_dims* d, int top_k) {
     return fail(PD_ERR_BAD_DIMS, "max_pages=%d must be at most %d to select pages", d->max_pages, kMaxSelectPages);
   if (top_k < 1 || top_k > d->max_pages)
     return fail(PD_ERR_BAD_DIMS, "top_k=%d must be in 1..max_pages=%d", top_k, d->max_pages);
-  if ((long long)d->batch * d->n_heads_kv * d->max_pages >= kMaxGrid)
-    return fail(PD_ERR_BAD_DIMS, "batch*n_heads_kv*max_pages must stay below 2^31 to select pages");
+  if ((double)d->batch * d->n_heads_kv * d->max_pages * pd::page_score_shares(sizes_of(d)) >= (double)kMaxGrid)
+    return fail(PD_ERR_BAD_DIMS, "selection of batch=%d over %d pages is too large for one launch", d->batch,
+                d->max_pages);
   return PD_OK;
 }
 
@@ -287,7 +295,9 @@ pd_status pd_paged_select(const pd_paged_dims* d, const pd_paged_cache* cache, c
   a.score = (double*)workspace;
   a.by_group = pd::fast_div(a.c.G);
   a.by_heads = pd::fast_div(a.c.Hkv);
+  a.shares = pd::page_score_shares(a.c);
   a.by_blocks = pd::fast_div(pd::page_score_blocks(a.c));
+  a.by_shares = pd::fast_div(a.shares);
   return hip_status(pd::launch_paged_select(a, (hipStream_t)stream), "page selection kernels");
 }
 

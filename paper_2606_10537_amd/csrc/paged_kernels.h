@@ -69,10 +69,12 @@ struct PageSelectArgs {
   const void* q;
   int top_k, n_first, n_last;
   int32_t* page_idx;
-  double* score;         // [B][H_kv][max_pages] workspace
-  FastDiv by_group, by_heads, by_blocks;   // G, H_kv, workgroups of a (sequence, head)
+  double* score;         // [B][H_kv][shares][max_pages] workspace
+  int shares;            // page_score_shares
+  FastDiv by_group, by_heads, by_blocks, by_shares;   // G, H_kv, workgroups of a share, shares
 };
-int page_score_blocks(const PagedArgs& p);   // workgroups that score the pages of one (sequence, head)
+int page_score_blocks(const PagedArgs& p);   // workgroups that score the pages of one (sequence, head, share)
+int page_score_shares(const PagedArgs& p);   // shares of its query rows
 hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s);
 
 // Rows of one query block: the query rows of a (sequence, KV head) are taken in

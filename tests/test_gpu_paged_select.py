@@ -41,7 +41,8 @@ def want(case, top_k, first, last):
 @pytest.mark.parametrize("dtype,cache", [(PD_BF16, PD_BF16), (PD_BF16, PD_FP8_E4M3), (PD_FP32, PD_FP32)])
 @pytest.mark.parametrize("hq,hkv,d,R,L,lens,k,first,last", [
     (4, 2, 64, 16, 1, [200, 16, 0, 1, 500], 5, 1, 2), (8, 1, 128, 16, 1, [3000], 17, 0, 0),
-    (6, 3, 128, 32, 3, [700, 90], 4, 0, 1), (34, 2, 64, 16, 2, [260, 250], 3, 2, 2), (1, 1, 64, 16, 1, [64], 4, 9, 9)])
+    (6, 3, 128, 32, 3, [700, 90], 4, 0, 1), (34, 2, 64, 16, 2, [260, 250], 3, 2, 2), (1, 1, 64, 16, 1, [64], 4, 9, 9),
+    (8, 1, 128, 16, 33, [300, 40, 33], 6, 0, 1), (12, 2, 64, 16, 9, [5000, 100], 40, 1, 0)])
 def test_pages_and_their_attention(gpu_lib, dtype, cache, hq, hkv, d, R, L, lens, k, first, last):
     print(f"[select] {dtype}/{cache} {hq}/{hkv} d={d} R={R} L={L} {lens} top {k}", flush=True)
     new = [min(L, n) for n in lens]
