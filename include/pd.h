@@ -437,8 +437,12 @@ pd_status pd_paged_select(const pd_paged_dims *dims, const pd_paged_cache *cache
  * sees no position, or only scores of -inf, gets o = 0 and lse = -inf.  What
  * the pages hold behind kv_len is never used, whatever its bits.  A page id
  * outside 0..n_pages-1 that is needed makes the group's rows NaN.
+ * The weights are rounded to bf16 before they multiply V with dtype = PD_BF16
+ * (their sum, and so lse, is taken before); sums are fp32 and divided at the
+ * end, so they overflow where 256 * sum |v| over the visible keys passes 2^128.
  * The lengths are known on the device alone: the split of long sequences over
  * workgroups, and their join, are planned there.
+ * Exponent bytes are those that pd_paged_append writes.
  * workspace: >= pd_paged_workspace_bytes(dims, top_k, 1) bytes (may be 0, then
  * workspace may be NULL).
  */

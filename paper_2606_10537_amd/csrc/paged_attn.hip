@@ -8,10 +8,16 @@
 // * A wave takes 32 keys (fp32: 16) a step, loads the next step's K and V straight into
 //   registers while it works on this one, and keeps a softmax of its own; four waves
 //   of a workgroup walk neighbouring steps and are joined through LDS at the end.
-//   No barrier and no LDS in the loop.
+//   No barrier in the loop, and no LDS (but for values that are not finite).
 // * The keys of all sequences are cut into parts of nearly one size (plan below),
 //   planned on the device from the lengths, so that ragged batches fill the card
 //   evenly; rows whose keys are cut are joined by a second kernel.
+//
+// Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 345 us, 6.3 TB/s; 64 ragged sequences of up to
+// 32K, 8 heads, 8 bits, pages of 16 rows 370 us, 5.9 TB/s.  One token of one 8K sequence takes 7.2 +
+// 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
+// every CU has one.
 //
 // Operand layouts (lane = 16 g + n).  16x16x32 bf16: A holds row n, B column n, both
 // at k = 8 g .. 8 g + 7; the result's element e is row 4 g + e of column n.
@@ -51,9 +57,9 @@ struct PagedPart {
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
 // card at once are cut into as few parts as give every CU one.  Otherwise parts of 16 blocks
 // or more, paged_parts of them where the keys suffice, so that the workgroups of short
-// sequences and the ends of long ones fill in.  Measured, 2 CU-filling parts against 8: 8 x 32
-// heads x 8K keys 170 against 179 us, 8 x 8 heads x 32K 175 against 188, 64 ragged
-// sequences in 8 bits 474 against 382 us.
+// sequences and the ends of long ones fill in.  Measured: 8 x 32
+// heads x 8K keys 160 us, 174 in such finer parts; 8 x 8 heads x 32K 169 and 172; 64 ragged sequences
+// in 8 bits 379 us in finer parts, 474 in as few as the CUs.
 struct PagedSeq {
   int len, n_new, blocks;
 };
@@ -234,8 +240,9 @@ __device__ __forceinline__ T fetch(const T* p) {
 
 constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 
-// STREAM: the keys are read by one workgroup alone (non-temporal loads: 8 x 32K keys 654
-// against 718 us); row blocks that share them leave them in the caches.
+// STREAM: the keys are read by one workgroup alone (non-temporal loads: 8 x 32 heads x 32K keys 648
+// against 723 us, 64 ragged sequences in 8 bits 381 against 402); row blocks that share them leave
+// them in the caches.
 template <int D, int CT, int RT, bool STREAM>
 __global__ __launch_bounds__(256, RT == 1 || D == 64 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
@@ -637,8 +644,7 @@ __global__ __launch_bounds__(256, RT == 1 || D == 64 ? 2 : 1) void paged_attn_ke
 // parts' order.  A thread takes four channels of every SL-th part, with the loads of eight
 // parts in flight, and the slices are joined through LDS.  RW rows a workgroup: one where
 // there are few rows, which may have many parts each; four where there are many rows and
-// so few parts (rows of one part only end sooner then: 13 x 16 heads x 33 rows 3.0 us, one a
-// workgroup 5.6).
+// so few parts, or one, each (a call of 13 x 16 heads x 33 rows 22.2 us, 23.6 with one row a workgroup).
 template <int D, bool BF16, int RW>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   constexpr int T = D / 4, SL = 256 / T / RW, U = 8;   // threads of a row, slices of the parts

@@ -160,6 +160,26 @@ def test_bad_pages_give_nan(gpu_lib):
         assert torch.isnan(run_attn(case, c)[0][1]).all()
 
 
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
+@pytest.mark.parametrize("causal", [0, 1])
+def test_more_new_rows_than_positions(gpu_lib, dtype, cache, causal):
+    """Lengths below the number of new rows: the rows whose position lies before 0 see nothing (causal); lengths and
+    counts beyond their bounds, below and above, count as the bounds."""
+    case = Case([3, 64, 40], new_len=5, hq=4, hkv=2, d=64, dtype=dtype, cache=cache, R=16, causal=causal, seed=4)
+    c = case.to_gpu()
+    o, lse = run_attn(case, c)
+    if causal:
+        assert torch.all(o[0, :2] == 0) and torch.all(lse[0, :, :2] == -math.inf)
+    check_attn(case, o, lse)
+    c["kv_len"].copy_(torch.tensor([-9, 1 << 30, 40], dtype=torch.int32))
+    c["new_rows"].copy_(torch.tensor([5, 1 << 30, -1], dtype=torch.int32))
+    o, lse = run_attn(case, c)
+    assert torch.all(o[0] == 0) and torch.all(lse[0] == -math.inf) and torch.all(o[2] == 7) and torch.all(lse[2] == 7)
+    case.lens, case.new = [0, 64, 40], [5, 5, 0]
+    case.held = {n: [case.held[n][0][:0], *case.held[n][1:]] for n in case.held}
+    check_attn(case, o, lse)
+
+
 def test_softmax_scale(gpu_lib):
     case = Case([77], hq=2, hkv=1, d=128, R=16, seed=5, sm_scale=0.3)
     check_attn(case, *run_attn(case, case.to_gpu()))
