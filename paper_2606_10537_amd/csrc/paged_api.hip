@@ -331,6 +331,7 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.by_heads = pd::fast_div(a.c.Hkv);
   a.by_rows = pd::fast_div(a.c.G * a.c.Ln);
   a.by_blocks = pd::fast_div(a.row_blocks);
+  a.by_units = pd::fast_div(a.c.Hkv * a.row_blocks);
   return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");
 }
 

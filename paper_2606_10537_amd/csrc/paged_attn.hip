@@ -93,29 +93,56 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   const int units = p.Hkv * a.row_blocks;
   auto add = [](int x, int y) { return x + y; };
   auto larger = [](int x, int y) { return max(x, y); };
-  const PagedSeq head = paged_seq<BK>(a, lane);
-  int quota = 1 << 30;
-  bool even = true;
-  if (a.max_chunks > 1) {
-    // In fp32, which a quota need not be exact for: an error of 2^-12 in it still leaves the
-    // number of parts below what the host has made room for.
-    float all = 0.f;
-    int most = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64) {
-      const int n = b0 == 0 ? head.blocks : paged_seq<BK>(a, b0 + lane).blocks;
-      all += (float)__builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
-      most = max(most, __builtin_amdgcn_readlane(wave_scan(n, 0, larger), 63));
+  PagedPart r{};
+  // Number i among a sequence's parts of this turn, `each` a unit: head and part, and row block.  Row
+  // blocks of the same keys run on one XCD, eight workgroups apart, so that all but the first find
+  // them in its L2.
+  auto place = [&](int i, int each) {
+    int pair = i;
+    r.rb = 0;
+    if (a.row_blocks > 1) {
+      if (i < p.Hkv * each / kNumXcd * kNumXcd * a.row_blocks) {
+        const int q = a.by_blocks.quot(i / kNumXcd);
+        r.rb = a.by_blocks.rem(i / kNumXcd, q);
+        pair = q * kNumXcd + i % kNumXcd;
+      } else {
+        pair = a.by_blocks.quot(i);
+        r.rb = a.by_blocks.rem(i, pair);
+      }
     }
-    const float seqs = (float)p.B * (float)units;
-    all *= (float)units;
-    auto ceil_of = [](float x) {
-      const int c = (int)fminf(x, 1073741824.f);
-      return (float)c < x ? c + 1 : c;
-    };
-    const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
-    even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
-    quota = max(1, uniform(even ? fill : max(fine, min(fill, 16))));
+    return pair;
+  };
+  if (a.max_chunks == 1) {   // one part a unit
+    r.b = a.by_units.quot(find);
+    if (r.b >= p.B) return r;
+    const PagedSeq s = paged_seq<BK>(a, r.b);
+    r.len = s.len;
+    r.n_new = s.n_new;
+    r.g = place(a.by_units.rem(find, r.b), 1);
+    r.last = s.blocks;
+    r.parts = 1;
+    r.any = true;
+    return r;
   }
+  const PagedSeq head = paged_seq<BK>(a, lane);
+  // In fp32, which a quota need not be exact for: an error of 2^-12 in it still leaves the
+  // number of parts below what the host has made room for.
+  float all = 0.f;
+  int most = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int n = b0 == 0 ? head.blocks : paged_seq<BK>(a, b0 + lane).blocks;
+    all += (float)__builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
+    most = max(most, __builtin_amdgcn_readlane(wave_scan(n, 0, larger), 63));
+  }
+  const float seqs = (float)p.B * (float)units;
+  all *= (float)units;
+  auto ceil_of = [](float x) {
+    const int c = (int)fminf(x, 1073741824.f);
+    return (float)c < x ? c + 1 : c;
+  };
+  const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
+  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
+  const int quota = max(1, uniform(even ? fill : max(fine, min(fill, 16))));
   // Order: the parts of a whole quota, then the shorter ends, which even out when the
   // workgroups finish.  `whole` of a sequence's `parts` come in the first turn.
   struct Cut {
@@ -139,7 +166,6 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   }
   const bool second = find >= first_turn;
   if (second) find -= first_turn;
-  PagedPart r{};
   int before = 0, before_all = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const PagedSeq s = b0 == 0 ? head : paged_seq<BK>(a, b0 + lane);
@@ -157,21 +183,7 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       r.parts = __builtin_amdgcn_readlane(c.parts, l);
       const int mine = __builtin_amdgcn_readlane(own, l);
       const int each = second ? 1 : __builtin_amdgcn_readlane(c.whole, l);   // of a unit in this turn
-      // Row blocks of the same keys run on one XCD, eight workgroups apart, so that all but
-      // the first find them in its L2.
-      const int i = find - (__builtin_amdgcn_readlane(incl, l) - mine);
-      int pair = i;
-      r.rb = 0;
-      if (a.row_blocks > 1) {
-        if (i < p.Hkv * each / kNumXcd * kNumXcd * a.row_blocks) {
-          const int q = a.by_blocks.quot(i / kNumXcd);
-          r.rb = a.by_blocks.rem(i / kNumXcd, q);
-          pair = q * kNumXcd + i % kNumXcd;
-        } else {
-          pair = a.by_blocks.quot(i);
-          r.rb = a.by_blocks.rem(i, pair);
-        }
-      }
+      const int pair = place(find - (__builtin_amdgcn_readlane(incl, l) - mine), each);
       r.g = pair;
       r.index = second ? r.parts - 1 : 0;
       if (each > 1) {
@@ -244,7 +256,7 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 // against 723 us, 64 ragged sequences in 8 bits 381 against 402); row blocks that share them leave
 // them in the caches.
 template <int D, int CT, int RT, bool STREAM>
-__global__ __launch_bounds__(256, RT == 1 || D == 64 ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
@@ -254,7 +266,7 @@ __global__ __launch_bounds__(256, RT == 1 || D == 64 ? 2 : 1) void paged_attn_ke
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
   const PagedPart part = paged_find<BK>(a, uniform((int)block_id()), lane);
   if (!part.any) return;
-  const int b = uniform(part.b), g = uniform(part.g), len = part.len, n_new = part.n_new;
+  const int b = uniform(part.b), g = uniform(part.g), len = uniform(part.len), n_new = uniform(part.n_new);
   const int rows = n_new * p.G, row0 = uniform(part.rb) * (RT * 16);
   if (a.max_chunks > 1 && part.index == 0 && threadIdx.x == 0) {   // what the join has to know of the unit
     int32_t* u = a.unit + (((long long)b * p.Hkv + g) * a.row_blocks + part.rb) * 4;

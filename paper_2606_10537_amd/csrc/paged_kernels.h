@@ -95,7 +95,7 @@ struct PagedAttnArgs {
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
   long long grid;
-  FastDiv by_group, by_heads, by_rows, by_blocks;  // G, H_kv, G * L_n, row_blocks
+  FastDiv by_group, by_heads, by_rows, by_blocks, by_units;  // G, H_kv, G * L_n, row_blocks, H_kv * row_blocks
 };
 // Parts that the keys of a ragged batch are cut into at most, besides one for every unit, for
 // `rows` query rows of a KV head.  How many there are is known on the device alone, so as many

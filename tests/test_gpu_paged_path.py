@@ -236,3 +236,57 @@ def test_binding_refuses_what_does_not_fit(gpu_lib):
     with pytest.raises(_lib.PdError):
         _lib.pd_paged_read(d, c["cache"], 0, 49, *(torch.zeros(2, 2, 49, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)))
     torch.cuda.synchronize()
+
+
+def test_no_launch_beside_the_current_device(gpu_lib):
+    with pytest.raises(ValueError, match="current"):
+        _lib._launch_stream(None, torch.cuda.current_device() + 1)
+
+
+def test_grids_beyond_one_dimension(gpu_lib):
+    """More than 2^20 workgroups in every launch: 5 million rows of one head normalised and rotated, and a token of
+    40000 sequences of 32 heads, all with the same page contents, appended, chosen from, attended to and read back."""
+    T, d = 5_000_000, 64
+    x = torch.randn(T, 1, d, device="cuda").to(torch.bfloat16)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    y = torch.empty_like(x)
+    _lib.pd_qk_norm_rope(x, None, None, None, 0.0, pos, 1e4, y, None)
+    at = torch.tensor([0, 1, 4_194_303, 4_194_304, T - 1], device="cuda")
+    want = ref.qk_norm_rope_ref(h64(x[at]), None, 0, h64(pos[at]), 1e4)
+    assert np.all(np.abs(h64(y[at]) - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * 8)
+    assert torch.allclose(y.float().norm(dim=-1), x.float().norm(dim=-1), rtol=2.0 ** -7)    # turned, not stretched
+    del x, y
+    B, H, R = 40000, 32, 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    row = lambda h: torch.randn(1, 1, h, d, generator=g, device="cuda").to(torch.bfloat16).expand(B, 1, h, d).contiguous()  # noqa: E731
+    dims = _lib.PagedDims(batch=B, new_len=1, n_heads_q=H, n_heads_kv=H, head_dim=d, dtype=PD_BF16, cache_dtype=PD_BF16,
+                          page_rows=R, n_pages=B, max_pages=1, causal=1)
+    k, v = (torch.zeros(B, H, R, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    bounds = torch.zeros(B, H, 2, d, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(B - 1, -1, -1, dtype=torch.int32, device="cuda").view(B, 1)
+    kv_len = torch.zeros(B, dtype=torch.int32, device="cuda")
+    cache = _lib.PagedCache(dims, k, v, table, kv_len, k_bounds=bounds)
+    rows = []
+    for _ in range(3):
+        kv_len.add_(1)
+        rows.append((row(H), row(H)))
+        _lib.pd_paged_append(dims, cache, *rows[-1])
+    assert torch.equal(k, k[:1].expand_as(k)) and torch.equal(bounds, bounds[:1].expand_as(bounds))
+    assert torch.equal(v[0, :, :3], torch.cat([r[1][0] for r in rows]).transpose(0, 1))
+    q, idx = row(H), torch.empty(B, H, 1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(_lib.pd_paged_workspace_bytes(dims, 1, 0), 16), dtype=torch.uint8, device="cuda")
+    _lib.pd_paged_select(dims, cache, q, 1, 0, 0, idx, ws)
+    assert torch.all(idx == 0)
+    assert _lib.pd_paged_workspace_bytes(dims, 1, 1) == 0
+    o, lse = torch.empty_like(q), torch.empty(B, H, 1, device="cuda")
+    for sel in (None, idx):
+        o.zero_()
+        _lib.pd_paged_attn(dims, cache, q, o, lse, page_idx=sel)
+        assert torch.equal(o, o[:1].expand_as(o)) and torch.equal(lse, lse[:1].expand_as(lse))
+        for h in (0, 17, 31):
+            want, l, mass, _ = ref.attn_ref(h64(q[0, :, h]), h64(k[0, h, :3]), h64(v[0, h, :3]), [3], d ** -0.5)
+            assert np.all(np.abs(h64(o[0, :, h]) - want) <= 2.0 ** -8 * (mass + np.abs(want)) + 2.0 ** -17 * mass)
+            assert abs(lse[0, h, 0].item() - l[0]) < 1e-5
+    out = [torch.empty(B, H, 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    _lib.pd_paged_read(dims, cache, 1, 2, *out)
+    assert torch.equal(out[0], out[0][:1].expand_as(out[0])) and torch.equal(out[0][0], k[0, :, 1:3])
