@@ -14,8 +14,8 @@
 //   evenly; rows whose keys are cut are joined by a second kernel.
 //
 // Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
-// nothing but read reaches 6.5 to 7.1 here); in 8 bits 345 us, 6.3 TB/s; 64 ragged sequences of up to
-// 32K, 8 heads, 8 bits, pages of 16 rows 370 us, 5.9 TB/s.  One token of one 8K sequence takes 7.2 +
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 335 us, 6.4 TB/s; 64 ragged sequences of up to
+// 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s.  One token of one 8K sequence takes 7.2 +
 // 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
 // every CU has one.
 //
@@ -26,7 +26,8 @@
 //     16 keys (j < 4) or 4 g + j - 4 of its second, so the result of S^T is P^T
 //     as it stands.  A lane reads E = D / 16 neighbouring channels of its eight keys,
 //     16 lanes a whole row; a byte permutation of register pairs turns the
-//     8 x E block into the A operands of E products.  Row m of product t is channel E m + t.
+//     8 x E block into the A operands of E products.  Row m of product t is channel base(m) + t,
+//     E m + t in bf16.
 // 16x16x4 fp32: k = g, one value a lane; four products per 16-byte read, and the
 // channels of a read are permuted alike in both operands.
 #include <type_traits>
@@ -59,7 +60,7 @@ struct PagedPart {
 // or more, paged_parts of them where the keys suffice, so that the workgroups of short
 // sequences and the ends of long ones fill in.  Measured: 8 x 32
 // heads x 8K keys 160 us, 174 in such finer parts; 8 x 8 heads x 32K 169 and 172; 64 ragged sequences
-// in 8 bits 379 us in finer parts, 474 in as few as the CUs.
+// in 8 bits 365 us in finer parts, 474 in as few as the CUs.
 struct PagedSeq {
   int len, n_new, blocks;
 };
@@ -214,6 +215,8 @@ struct PagedShape {
   static constexpr int VW = D * CB / 64;                    // dwords of each
   static constexpr int E = CT == kFp32 ? 4 : D / 16;        // neighbouring channels of a lane
   static constexpr int NT = D / 16;                         // products of P V
+  // First channel of result row m (bf16 and E4M3).
+  static __device__ __forceinline__ int base(int m) { return CT == kFp8 ? 2 * E * (m & 7) + E * (m >> 3) : E * m; }
   static constexpr int BK = kPagedWaves * KS;
 };
 
@@ -222,8 +225,8 @@ template <int D, int CT>
 struct PagedStep {
   using S = PagedShape<D, CT>;
   u32x4 k[S::H][S::NK];
-  uint32_t v[S::VR][S::VW];
-  uint32_t ke[S::H], ve[S::H];   // exponent bytes of keys 4 g .. 4 g + 3
+  uint32_t v[S::VR][S::VW];      // E4M3: read 2 j + i of 16 keys, rows 2 j and 2 j + 1 in a line
+  uint32_t ex;                   // exponent bytes of four keys (see load)
   int pos[S::H];                 // position of the first key of each 16
 };
 
@@ -242,6 +245,16 @@ __device__ __forceinline__ float group_max(float x) {
 }
 __device__ __forceinline__ float group_sum(float x) {
   return over_groups(x, [](float a, float b) { return a + b; });
+}
+
+template <int CTRL, int BANKS>
+__device__ __forceinline__ uint32_t dpp_bits(uint32_t old, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, 0xf, BANKS, false);
+}
+// The value of lane L + h of the own row of 16 lanes.
+template <int L>
+__device__ __forceinline__ uint32_t row_lane(uint32_t x, int h) {
+  return h == 0 ? dpp_bits<0x150 + L, 0xf>(x, x) : dpp_bits<0x151 + L, 0xf>(x, x);   // row_newbcast
 }
 
 template <bool STREAM, class T>
@@ -343,6 +356,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
 
   const uint32_t page_rows = (uint32_t)p.R;
   auto load = [&](PagedStep<D, CT>& s, int i) {
+    long long rows_at[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       const int page = __builtin_amdgcn_readlane(at_page[h], i & 63);
@@ -352,26 +366,38 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
 #pragma unroll
       for (int j = 0; j < NK; ++j) s.k[h][j] = fetch<STREAM>((const u32x4*)(kp + 64 * j));
       const char* vp = (const char*)p.v_pages + row * (D * CB) + g4 * (4 * D * CB);
-      // fp32: channels 64 u + 4 n.., u = 0..D/64-1; otherwise E n..
+      if constexpr (CT == kFp8) {
+        // Lanes n and n ^ 8 read twice the channels that they need, of two keys each, and swap
+        // halves later: loads of 8 bytes a lane were twice as many (one sequence of 128K keys
+        // with 8 heads 50.8 us, now 49.0; 64 ragged ones 380, now 377).
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t* w = s.v[4 * h + j];
-        if constexpr (CT == kFp32) {
+        for (int j = 0; j < 2; ++j) {
+          uint32_t* w = s.v[4 * h + 2 * j];
+          const char* at = vp + (2 * (n >> 3) + j) * D + (n & 7) * (D / 8);
+          if constexpr (VW == 2) *(u32x4*)w = fetch<STREAM>((const u32x4*)at);
+          else *(u32x2*)w = fetch<STREAM>((const u32x2*)at);
+        }
+      } else {
+        // fp32: channels 64 u + 4 n.., u = 0..D/64-1; bf16: E n..
 #pragma unroll
-          for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
-        } else if constexpr (VW == 4) {
-          *(u32x4*)w = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 16 * n));
-        } else if constexpr (VW == 2) {
-          *(u32x2*)w = fetch<STREAM>((const u32x2*)(vp + j * (D * CB) + 8 * n));
-        } else {
-          *w = fetch<STREAM>((const uint32_t*)(vp + j * (D * CB) + 4 * n));
+        for (int j = 0; j < 4; ++j) {
+          uint32_t* w = s.v[4 * h + j];
+          if constexpr (CT == kFp32) {
+#pragma unroll
+            for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
+          } else if constexpr (VW == 4) {
+            *(u32x4*)w = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 16 * n));
+          } else {
+            *(u32x2*)w = fetch<STREAM>((const u32x2*)(vp + j * (D * CB) + 8 * n));
+          }
         }
       }
-      if constexpr (CT == kFp8) {
-        s.ke[h] = *(const uint32_t*)(p.k_exp + row + 4 * g4);
-        s.ve[h] = *(const uint32_t*)(p.v_exp + row + 4 * g4);
-      }
+      rows_at[h] = row;
     }
+    // One load of all exponent bytes: keys 4 g.. of K's first 16 in lanes n = 0 (mod 4), of its
+    // second in 1, of V's in 2 and 3.
+    if constexpr (CT == kFp8)
+      s.ex = *(const uint32_t*)((n & 2 ? p.v_exp : p.k_exp) + (n & 1 ? rows_at[H - 1] : rows_at[0]) + 4 * g4);
   };
 
   // whole: every row sees every key of the step.
@@ -380,19 +406,32 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
     // Values as bf16 (or fp32), zeros where no key is: a weight of zero does not cancel
     // an infinity or a NaN.
     constexpr int W = CT == kFp32 ? VW : D / 32;
-    uint32_t v[VR][W];
+    uint32_t v[VR][W], ke[H], ve[H];
+    if constexpr (CT == kFp8) {
 #pragma unroll
-    for (int j = 0; j < VR; ++j) {
-      if constexpr (CT == kFp8) {
+      for (int h = 0; h < H; ++h) {
+        ke[h] = row_lane<0>(s.ex, h);
+        ve[h] = row_lane<2>(s.ex, h);
+      }
 #pragma unroll
-        for (int w = 0; w < VW; ++w) {
-          v[j][2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.v[j][w], 1.0f, false));
-          v[j][2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(s.v[j][w], 1.0f, true));
-        }
-      } else {
+      for (int j = 0; j < VR; j += 4)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int w = 0; w < VW; ++w) {
+            // lanes 0..7 hold keys 0 and 1, 8..15 keys 2 and 3; the lower keep the lower channels
+            const uint32_t lo = s.v[j + 2 * i][w], hi = s.v[j + 2 * i + 1][w];
+            const uint32_t x = dpp_bits<0x128, 0xc>(lo, hi), y = dpp_bits<0x128, 0x3>(hi, lo);
+            v[j + i][2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+            v[j + i][2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true));
+            v[j + 2 + i][2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.0f, false));
+            v[j + 2 + i][2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, 1.0f, true));
+          }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VR; ++j)
 #pragma unroll
         for (int w = 0; w < W; ++w) v[j][w] = s.v[j][w];
-      }
     }
     if constexpr (!whole) {
 #pragma unroll
@@ -428,7 +467,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
 #pragma unroll
           for (int w = 0; w < W; ++w) {
             const int key = 16 * (j / 4) + 4 * g4 + j % 4;
-            const int at = CT == kFp32 ? 64 * (w / 4) + 4 * n + w % 4 : (E * n + 2 * w) / 2;
+            const int at = CT == kFp32 ? 64 * (w / 4) + 4 * n + w % 4 : (S::base(n) + 2 * w) / 2;
             copy[key * (CT == kFp32 ? D : D / 2) + at] = v[j][w];
             if constexpr (CT == kFp32) {
               if (!(fabsf(__uint_as_float(v[j][w])) < INFINITY)) v[j][w] = 0u;
@@ -476,7 +515,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float x = sc[h][e] * p.scale_log2;
-          if constexpr (CT == kFp8) x *= exp_to_scale((s.ke[h] >> (8 * e)) & 255);
+          if constexpr (CT == kFp8) x *= exp_to_scale((ke[h] >> (8 * e)) & 255);
           if (!whole) x = s.pos[h] + 4 * g4 + e < lim[t] ? x : -INFINITY;
           sc[h][e] = x;
           top = fmaxf(top, x);
@@ -499,7 +538,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
           float x = fast_exp2(sc[h][e] - m[t]);
           l[t] += x;
           if constexpr (CT == kFp8) {
-            x *= exp_to_scale((s.ve[h] >> (8 * e)) & 255);
+            x *= exp_to_scale((ve[h] >> (8 * e)) & 255);
             if (!whole) x = s.pos[h] + 4 * g4 + e < lim[t] ? x : 0.f;   // bytes that no row wrote
           }
           pr[h][e] = x;
@@ -531,7 +570,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-              const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : E * (4 * g4 + r) + i;
+              const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : S::base(4 * g4 + r) + i;
               const uint32_t u = __float_as_uint(copy[CT == kFp32 ? ch : ch / 2]);
               const float x = __uint_as_float(CT == kFp32 ? u : i & 1 ? u & 0xffff0000u : u << 16);
               if (!(fabsf(x) < INFINITY)) o[t][i][r] += x;
@@ -601,12 +640,12 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
 #pragma unroll
     for (int w = 1; w < kPagedWaves; ++w) top = fmaxf(top, lds_ml[w][t * 16 + n][0]);
     const float f = fast_exp2(m[t] - top);
-    // fp32: product 4 u + e has channel 64 u + 4 (4 g + r) + e, otherwise t has E (4 g + r) + t.
+    // fp32: product 4 u + e has channel 64 u + 4 (4 g + r) + e, otherwise t has base(4 g + r) + t.
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
       for (int i = 0; i < NT; i += 4) {
-        const int ch = CT == kFp32 ? 16 * i + 4 * (4 * g4 + r) : E * (4 * g4 + r) + i;
+        const int ch = CT == kFp32 ? 16 * i + 4 * (4 * g4 + r) : S::base(4 * g4 + r) + i;
         *(f32x4*)&lds_o[wave][n][ch] = f32x4{o[t][i][r], o[t][i + 1][r], o[t][i + 2][r], o[t][i + 3][r]} * f;
       }
     __syncthreads();

@@ -100,9 +100,10 @@ struct PagedAttnArgs {
 // Parts that the keys of a ragged batch are cut into at most, besides one for every unit, for
 // `rows` query rows of a KV head.  How many there are is known on the device alone, so as many
 // workgroups are launched, and one that finds no part costs its launch: little where a CU
-// holds two or more, but 4 us for a thousand of those with more than 16 rows, of which it holds
-// one (8 rows of 4 heads over 8 x 8K keys 53.5 us with 2048, 57.5 with 3072).
-inline int paged_parts(long long rows) { return rows <= 16 ? 3072 : 1024; }
+// holds two or more (64 ragged requests in 8 bits 371 us with 2048, 362 with 3328, 367 with
+// 4096), but 4 us for a thousand of those with more than 16 rows, of which it holds one
+// (8 rows of 4 heads over 8 x 8K keys 51.2 us with 1024, 54.1 with 2048, 56.5 with 2900).
+inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
