@@ -113,7 +113,8 @@ long long touched_pages(const pd_paged_dims* d) {
 struct AttnPlan {
   int row_blocks, part_rows, parts, max_chunks;
   long long grid;
-  size_t o_bytes, ml_bytes, total;
+  size_t o_bytes, ml_bytes, unit_bytes, total;
+  bool planned;
 };
 pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   const long long rows = (long long)(d->n_heads_q / d->n_heads_kv) * d->new_len;
@@ -133,7 +134,10 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   const size_t slots = p->max_chunks == 1 ? 0 : (size_t)p->grid * p->part_rows;
   p->o_bytes = round_up(slots * d->head_dim * sizeof(float));
   p->ml_bytes = round_up(slots * 2 * sizeof(float));
-  p->total = p->o_bytes + p->ml_bytes + (slots ? round_up((size_t)units * 4 * sizeof(int32_t)) : 0);
+  p->unit_bytes = slots ? round_up((size_t)units * 4 * sizeof(int32_t)) : 0;
+  p->planned = slots && d->batch > pd::kPlanBatch;
+  p->total = p->o_bytes + p->ml_bytes + p->unit_bytes +
+             (p->planned ? round_up((4 + 2 * (size_t)cdiv(d->batch, 64)) * sizeof(int32_t)) : 0);
   return PD_OK;
 }
 
@@ -322,6 +326,7 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.o_part = (float*)workspace;
   a.ml_part = (float*)((char*)workspace + plan.o_bytes);
   a.unit = (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes);
+  a.plan = plan.planned ? (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes + plan.unit_bytes) : nullptr;
   a.row_blocks = plan.row_blocks;
   a.part_rows = plan.part_rows;
   a.max_chunks = plan.max_chunks;

@@ -53,7 +53,8 @@ struct PagedPart {
 // The cut of all sequences' keys.  Sequence b has n_b blocks of keys for each of its
 // units (KV head x row block).  With a quota of Q blocks a part, a unit has ceil(n_b / Q)
 // parts, the last one shorter; they are numbered by sequence, head and part.  Every
-// wave finds its own part from the lengths, 64 sequences at a time.
+// wave finds its own part from the lengths, 64 sequences at a time (large batches: from sums that a
+// launch before has left, paged_plan_kernel).
 //
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
 // card at once are cut into as few parts as give every CU one.  Otherwise parts of 16 blocks
@@ -88,12 +89,111 @@ __device__ __forceinline__ int parts_of(int blocks, int quota) {
   return blocks <= quota ? 1 : short_div(blocks - 1, quota) + 1;
 }
 
+// What is common to all parts.
+struct PagedQuota {
+  int quota;
+  bool even;
+};
+// all: the blocks of all units, in fp32, which a quota need not be exact for: an error of 2^-12
+// still leaves the number of parts below what the host has made room for.  most: of the longest.
+__device__ __forceinline__ PagedQuota paged_quota(const PagedAttnArgs& a, float all, int most) {
+  const float seqs = (float)a.c.B * (float)(a.c.Hkv * a.row_blocks);
+  auto ceil_of = [](float x) {
+    const int c = (int)fminf(x, 1073741824.f);
+    return (float)c < x ? c + 1 : c;
+  };
+  const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
+  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
+  return {max(1, uniform(even ? fill : max(fine, min(fill, 16)))), even};
+}
+// Order: the parts of a whole quota, then the shorter ends, which even out when the
+// workgroups finish.  `whole` of the parts of each of a sequence's units come in the first turn.
+struct PagedCut {
+  int parts, whole;
+};
+__device__ __forceinline__ PagedCut paged_cut(const PagedAttnArgs& a, const PagedQuota& q, int b, const PagedSeq& s) {
+  PagedCut c{0, 0};
+  if (b < a.c.B) {
+    c.parts = parts_of(s.blocks, q.quota);
+    c.whole = q.even || c.parts * q.quota == s.blocks ? c.parts : c.parts - 1;
+  }
+  return c;
+}
+__device__ __forceinline__ int wave_sum(int x) {
+  return __builtin_amdgcn_readlane(wave_scan(x, 0, [](int p, int q) { return p + q; }), 63);
+}
+__device__ __forceinline__ int wave_most(int x) {
+  return __builtin_amdgcn_readlane(wave_scan(x, 0, [](int p, int q) { return max(p, q); }), 63);
+}
+
+// The sums that every wave needs to find its part, for batches of more than kPlanBatch sequences,
+// where walking all lengths would cost each wave more than this launch: quota, whether the
+// batch is even, parts of the first turn, 0; then for every 64 sequences the parts of the
+// first turn, and of both, up to their end.  One workgroup.
+template <int BK>
+__global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
+  __shared__ float sums[16];
+  __shared__ int tops[16], whole[1024], parts[1024], ends[2][16];
+  const PagedArgs& p = a.c;
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  const int units = p.Hkv * a.row_blocks, n = (p.B + 63) / 64;   // at most 1024
+  float all = 0.f;
+  int most = 0;
+  for (int i = wave; i < n; i += 16) {
+    const int x = paged_seq<BK>(a, 64 * i + lane).blocks;
+    all += (float)wave_sum(x);
+    most = max(most, wave_most(x));
+  }
+  sums[wave] = all;
+  tops[wave] = most;
+  __syncthreads();
+  all = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    all += sums[w];
+    most = max(most, tops[w]);
+  }
+  const PagedQuota q = paged_quota(a, all * (float)units, most);
+  for (int i = wave; i < n; i += 16) {
+    const PagedCut c = paged_cut(a, q, 64 * i + lane, paged_seq<BK>(a, 64 * i + lane));
+    const int w = wave_sum(c.whole), x = wave_sum(c.parts);
+    if (lane == 0) {
+      whole[i] = w;
+      parts[i] = x;
+    }
+  }
+  __syncthreads();
+  auto add = [](int x, int y) { return x + y; };
+  int w = wave_scan(tid < n ? whole[tid] : 0, 0, add), x = wave_scan(tid < n ? parts[tid] : 0, 0, add);
+  if (lane == 63) {
+    ends[0][wave] = w;
+    ends[1][wave] = x;
+  }
+  __syncthreads();
+  int first = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    first += ends[0][i];
+    w += i < wave ? ends[0][i] : 0;
+    x += i < wave ? ends[1][i] : 0;
+  }
+  if (tid == 0) {
+    a.plan[0] = q.quota;
+    a.plan[1] = q.even;
+    a.plan[2] = first * units;
+    a.plan[3] = 0;
+  }
+  if (tid < n) {
+    a.plan[4 + 2 * tid] = w * units;
+    a.plan[5 + 2 * tid] = x * units;
+  }
+}
+
 template <int BK>
 __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find, int lane) {
   const PagedArgs& p = a.c;
   const int units = p.Hkv * a.row_blocks;
   auto add = [](int x, int y) { return x + y; };
-  auto larger = [](int x, int y) { return max(x, y); };
   PagedPart r{};
   // Number i among a sequence's parts of this turn, `each` a unit: head and part, and row block.  Row
   // blocks of the same keys run on one XCD, eight workgroups apart, so that all but the first find
@@ -125,55 +225,58 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
     r.any = true;
     return r;
   }
-  const PagedSeq head = paged_seq<BK>(a, lane);
-  // In fp32, which a quota need not be exact for: an error of 2^-12 in it still leaves the
-  // number of parts below what the host has made room for.
-  float all = 0.f;
-  int most = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const int n = b0 == 0 ? head.blocks : paged_seq<BK>(a, b0 + lane).blocks;
-    all += (float)__builtin_amdgcn_readlane(wave_scan(n, 0, add), 63);
-    most = max(most, __builtin_amdgcn_readlane(wave_scan(n, 0, larger), 63));
-  }
-  const float seqs = (float)p.B * (float)units;
-  all *= (float)units;
-  auto ceil_of = [](float x) {
-    const int c = (int)fminf(x, 1073741824.f);
-    return (float)c < x ? c + 1 : c;
-  };
-  const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
-  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
-  const int quota = max(1, uniform(even ? fill : max(fine, min(fill, 16))));
-  // Order: the parts of a whole quota, then the shorter ends, which even out when the
-  // workgroups finish.  `whole` of a sequence's `parts` come in the first turn.
-  struct Cut {
-    int parts, whole;
-  };
-  auto cut = [&](int b, const PagedSeq& s) {
-    Cut c{0, 0};
-    if (b < p.B) {
-      c.parts = parts_of(s.blocks, quota);
-      c.whole = even || c.parts * quota == s.blocks ? c.parts : c.parts - 1;
+  PagedQuota q;
+  PagedSeq s;
+  int first_turn, b0 = 0, before = 0, before_all = 0;   // parts of the turn, and of both, before sequence b0
+  bool second;
+  if (a.plan) {
+    q = {a.plan[0], a.plan[1] != 0};
+    first_turn = a.plan[2];
+    second = find >= first_turn;
+    if (second) find -= first_turn;
+    const int n = (p.B + 63) / 64;
+    for (int i0 = 0;; i0 += 64) {
+      if (i0 >= n) return r;
+      const int i = min(i0 + lane, n - 1), w = a.plan[4 + 2 * i], x = a.plan[5 + 2 * i];
+      const int own = second ? x - w : w;
+      const uint64_t past = __ballot(own > find);
+      const int l = past ? __ffsll((unsigned long long)past) - 1 : 64;   // those before end at or below `find`
+      if (l > 0) {
+        before = __builtin_amdgcn_readlane(own, l - 1);
+        before_all = __builtin_amdgcn_readlane(x, l - 1);
+      }
+      if (past) {
+        b0 = (i0 + l) * 64;
+        break;
+      }
     }
-    return c;
-  };
-  int first_turn = 0x7fffffff;
-  if (!even) {
-    first_turn = 0;
-    for (int b0 = 0; b0 < p.B; b0 += 64)
-      first_turn += __builtin_amdgcn_readlane(
-          wave_scan(cut(b0 + lane, b0 == 0 ? head : paged_seq<BK>(a, b0 + lane)).whole, 0, add), 63);
-    first_turn *= units;
+    s = paged_seq<BK>(a, b0 + lane);
+  } else {
+    const PagedSeq head = s = paged_seq<BK>(a, lane);
+    float all = 0.f;
+    int most = 0;
+    for (int c0 = 0; c0 < p.B; c0 += 64) {
+      const int n = c0 == 0 ? head.blocks : paged_seq<BK>(a, c0 + lane).blocks;
+      all += (float)wave_sum(n);
+      most = max(most, wave_most(n));
+    }
+    q = paged_quota(a, all * (float)units, most);
+    first_turn = 0x7fffffff;
+    if (!q.even) {
+      first_turn = 0;
+      for (int c0 = 0; c0 < p.B; c0 += 64)
+        first_turn += wave_sum(paged_cut(a, q, c0 + lane, c0 == 0 ? head : paged_seq<BK>(a, c0 + lane)).whole);
+      first_turn *= units;
+    }
+    second = find >= first_turn;
+    if (second) find -= first_turn;
   }
-  const bool second = find >= first_turn;
-  if (second) find -= first_turn;
-  int before = 0, before_all = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64) {
-    const PagedSeq s = b0 == 0 ? head : paged_seq<BK>(a, b0 + lane);
-    const Cut c = cut(b0 + lane, s);
+  const int quota = q.quota;
+  for (;;) {
+    const PagedCut c = paged_cut(a, q, b0 + lane, s);
     const int own = (second ? c.parts - c.whole : c.whole) * units;
     const int incl = before + wave_scan(own, 0, add);
-    const int incl_all = even ? incl : before_all + wave_scan(c.parts * units, 0, add);
+    const int incl_all = q.even ? incl : before_all + wave_scan(c.parts * units, 0, add);
     const uint64_t past = __ballot(incl > find);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;
@@ -199,8 +302,10 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
     }
     before = __builtin_amdgcn_readlane(incl, 63);
     before_all = __builtin_amdgcn_readlane(incl_all, 63);
+    b0 += 64;
+    if (b0 >= p.B) return r;
+    s = paged_seq<BK>(a, b0 + lane);
   }
-  return r;
 }
 
 enum { kBf16 = 0, kFp8 = 1, kFp32 = 2 };
@@ -776,6 +881,11 @@ template <int D, int CT>
 hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   const dim3 grid = grid_xy(a.grid);
   const int rows = a.c.G * a.c.Ln;
+  if (a.plan) {
+    hipLaunchKernelGGL((paged_plan_kernel<PagedShape<D, CT>::BK>), dim3(1), dim3(1024), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1, true>), grid, dim3(256), 0, s, a);
   else if (rows <= kPagedRows) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, false>), grid, dim3(256), 0, s, a);

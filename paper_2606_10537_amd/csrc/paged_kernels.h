@@ -91,6 +91,7 @@ struct PagedAttnArgs {
   float* o_part;         // [slot][part_rows][D] sums of a workgroup whose keys are a part of its rows'
   float* ml_part;        // [slot][part_rows][2] their maximum (log2 domain) and weight sum
   int32_t* unit;         // [B][H_kv][row_blocks][4]: a unit's first part, parts and rows
+  int32_t* plan;         // nullptr, or 4 + 2 ceil(B / 64) sums of the batch (paged_plan_kernel)
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
@@ -104,6 +105,10 @@ struct PagedAttnArgs {
 // 4096), but 4 us for a thousand of those with more than 16 rows, of which it holds one
 // (8 rows of 4 heads over 8 x 8K keys 51.2 us with 1024, 54.1 with 2048, 56.5 with 2900).
 inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
+// Largest batch whose lengths every wave walks by itself; one launch more does it for larger
+// ones (walked and planned, ragged lengths, 8 heads: 128 sequences 110 and 109 us, 512 259 and 197,
+// 4096 3830 and 833; 65 sequences 64 and 68).
+constexpr int kPlanBatch = 128;
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);

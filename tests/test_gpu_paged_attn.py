@@ -66,6 +66,42 @@ def test_many_sequences(gpu_lib):
     run("many", lens, hq=2, hkv=1, d=64, R=32, seed=8, max_pages=300)
 
 
+@pytest.mark.parametrize("B", [129, 700, 4200])
+@pytest.mark.parametrize("kind", range(len(KINDS)))
+def test_batches_planned_by_a_launch_of_their_own(gpu_lib, kind, B):
+    """Ragged batches with empty sequences, sequences without new rows and one long sequence, at either end of the
+    batch; the same call in a graph follows other lengths."""
+    dtype, cache = KINDS[kind]
+    g = torch.Generator().manual_seed(B + kind)
+    lens = torch.randint(0, 40, (B,), generator=g).tolist()
+    lens[(0, B // 2, B - 1)[kind % 3]] = 5000
+    new = [int(n) for n in torch.randint(0, 4, (B,), generator=g)]
+    hq, hkv = ((4, 2), (12, 1), (3, 3))[kind % 3]                  # 12 rows, 36 (two row blocks) and 3
+    case = Case(lens, new_len=3, new=new, hq=hq, hkv=hkv, d=64, dtype=dtype, cache=cache, R=16, seed=B)
+    c = case.to_gpu()
+    o, lse = run_attn(case, c)
+    check_attn(case, o, lse)
+    if B != 700:
+        return
+    ws = torch.empty(_lib.pd_paged_workspace_bytes(case.dims, 0, 1), dtype=torch.uint8, device="cuda")
+    go, gl = torch.full_like(o, 7.0), torch.full_like(lse, 7.0)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _lib.pd_paged_attn(case.dims, c["cache"], c["q"], go, gl, workspace=ws)
+    for shift in (0, 100, 350):                                    # the sequences' rows in other places of the batch
+        turned = {n: c[n].roll(shift, 0) for n in ("kv_len", "new_rows", "table", "q")}
+        saved = {n: c[n].clone() for n in turned}
+        for n, x in turned.items():
+            c[n].copy_(x)
+        go.fill_(7.0)
+        graph.replay()
+        eager, _ = run_attn(case, c)
+        assert torch.equal(go, eager)
+        assert shift or torch.equal(go, o)
+        for n, x in saved.items():
+            c[n].copy_(x)
+
+
 @pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
 def test_longer_walk_than_one_window(gpu_lib, dtype, cache):
     """Enough sequences that one workgroup walks more than 64 steps of a wave."""
