@@ -57,9 +57,9 @@ struct PagedPart {
 // launch before has left, paged_plan_kernel).
 //
 // The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
-// card at once are cut into as few parts as give every CU one.  Otherwise parts of 16 blocks
-// or more, paged_parts of them where the keys suffice, so that the workgroups of short
-// sequences and the ends of long ones fill in.  Measured: 8 x 32
+// card at once are cut into as few parts as give every CU one, if those fit too (paged_slots).
+// Otherwise parts of 16 blocks or more, paged_parts of them where the keys suffice, so that the
+// workgroups of short sequences and the ends of long ones fill in.  Measured: 8 x 32
 // heads x 8K keys 160 us, 174 in such finer parts; 8 x 8 heads x 32K 169 and 172; 64 ragged sequences
 // in 8 bits 365 us in finer parts, 474 in as few as the CUs.
 struct PagedSeq {
@@ -103,7 +103,8 @@ __device__ __forceinline__ PagedQuota paged_quota(const PagedAttnArgs& a, float 
     return (float)c < x ? c + 1 : c;
   };
   const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
-  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu;
+  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu &&
+                    (float)parts_of(most, fill) * seqs <= a.slots;
   return {max(1, uniform(even ? fill : max(fine, min(fill, 16)))), even};
 }
 // Order: the parts of a whole quota, then the shorter ends, which even out when the

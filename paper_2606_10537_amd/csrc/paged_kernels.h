@@ -95,6 +95,7 @@ struct PagedAttnArgs {
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
+  float slots;           // paged_slots
   long long grid;
   FastDiv by_group, by_heads, by_rows, by_blocks, by_units;  // G, H_kv, G * L_n, row_blocks, H_kv * row_blocks
 };
@@ -105,6 +106,11 @@ struct PagedAttnArgs {
 // 4096), but 4 us for a thousand of those with more than 16 rows, of which it holds one
 // (8 rows of 4 heads over 8 x 8K keys 51.2 us with 1024, 54.1 with 2048, 56.5 with 2900).
 inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
+// Parts that run at once, as far as it matters: up to 16 rows memory bounds the parts of a CU
+// together, but with more rows each part takes its own time, and a second round of them
+// as long again (24 rows of 4 heads over 8 x 8K keys, 192 units in two parts each: 145 us, 99
+// in parts of 16 blocks; 7 x 32 heads, 32 rows 249 and 197).
+inline float paged_slots(long long rows, int d) { return rows <= 16 ? 1e9f : d == 128 ? 256.f : 512.f; }
 // Largest batch whose lengths every wave walks by itself; one launch more does it for larger
 // ones (walked and planned, ragged lengths, 8 heads: 128 sequences 110 and 109 us, 512 259 and 197,
 // 4096 3830 and 833; 65 sequences 64 and 68).
