@@ -127,7 +127,7 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
     return fail(PD_ERR_BAD_DIMS, "attention of batch=%d with new_len=%d is too large for one launch", d->batch,
                 d->new_len);
   p->parts = pd::paged_parts(rows);
-  p->max_chunks = (int)std::min<long long>(blocks, p->parts);
+  p->max_chunks = blocks <= pd::paged_whole_blocks(units) ? 1 : (int)std::min<long long>(blocks, p->parts);
   // The kernels cut with a quota of at least all blocks / parts: at most so many whole
   // quotas, and one part that is not whole for each unit.
   p->grid = p->max_chunks == 1 ? units : std::min(units + p->parts, units * p->max_chunks);

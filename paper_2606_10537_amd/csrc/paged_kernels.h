@@ -111,6 +111,11 @@ inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
 // as long again (24 rows of 4 heads over 8 x 8K keys, 192 units in two parts each: 145 us, 99
 // in parts of 16 blocks; 7 x 32 heads, 32 rows 249 and 197).
 inline float paged_slots(long long rows, int d) { return rows <= 16 ? 1e9f : d == 128 ? 256.f : 512.f; }
+// Blocks up to which no unit's keys are cut, and no join follows: 16 where the units alone fill
+// the card (32 ragged sequences of 8 heads, 8 new rows, up to 600 / 2048 keys: cut 26.3 and 44.5 us,
+// whole 16.4 and 36.8; 12 of 32 heads up to 4096 keys, cut 85, whole 95), 4 elsewhere (8 heads
+// x 256 / 512 keys 9.9 and 10.0, whole 6.6 and 8.4; x 1024 keys 9.9 and 15.6).
+inline int paged_whole_blocks(long long units) { return units >= 256 ? 16 : 4; }
 // Largest batch whose lengths every wave walks by itself; one launch more does it for larger
 // ones (walked and planned, ragged lengths, 8 heads: 128 sequences 110 and 109 us, 512 259 and 197,
 // 4096 3830 and 833; 65 sequences 64 and 68).

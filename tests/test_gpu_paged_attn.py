@@ -50,6 +50,20 @@ def test_several_new_rows(gpu_lib, dtype, cache, causal, L, new, hq, hkv, d):
 
 
 @pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("L,new,hq,hkv,d,copies", [(1, [1, 1, 1, 1, 1], 4, 4, 64, 1), (2, [2, 1, 0, 2, 1], 2, 2, 128, 1),
+                                                   (5, [5, 3, 1, 5, 0], 8, 2, 128, 1), (33, [33, 32, 1, 20, 33], 3, 1, 64, 1),
+                                                   (16, [16, 16, 7, 16, 1], 8, 1, 128, 1), (2, [2, 1, 0, 2, 1], 2, 2, 64, 30)])
+def test_tables_wider_than_the_sequences(gpu_lib, dtype, cache, causal, L, new, hq, hkv, d, copies):
+    """Whether a call cuts its keys goes by the table's width: short sequences under a wide table and under a narrow
+    one, and 300 units of them, which narrow tables of up to 2048 rows leave whole."""
+    lens = [max(L, 1), 130, 64, 600, 0] * copies
+    for width in (38, 400):
+        run("width", lens, new_len=L, new=new * copies, hq=hq, hkv=hkv, d=d, dtype=dtype, cache=cache, R=16, causal=causal,
+            seed=L, max_pages=width)
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
 @pytest.mark.parametrize("lens", [[9000], [5000, 3, 0, 2500], [1000] * 9])
 def test_split_keys(gpu_lib, dtype, cache, lens):
     """Long caches cut over many workgroups and joined, beside short and empty ones, and the same bits again."""
