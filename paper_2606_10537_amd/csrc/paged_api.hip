@@ -137,7 +137,7 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
   p->unit_bytes = slots ? round_up((size_t)units * 4 * sizeof(int32_t)) : 0;
   p->planned = slots && d->batch > pd::kPlanBatch;
   p->total = p->o_bytes + p->ml_bytes + p->unit_bytes +
-             (p->planned ? round_up((4 + 2 * (size_t)cdiv(d->batch, 64)) * sizeof(int32_t)) : 0);
+             (p->planned ? round_up((2 + 2 * (size_t)cdiv(d->batch, 64)) * sizeof(int32_t)) : 0);
   return PD_OK;
 }
 

@@ -56,12 +56,13 @@ struct PagedPart {
 // wave finds its own part from the lengths, 64 sequences at a time (large batches: from sums that a
 // launch before has left, paged_plan_kernel).
 //
-// The quota: units of one size (the longest at most 5/4 of the mean) that all fit on the
-// card at once are cut into as few parts as give every CU one, if those fit too (paged_slots).
-// Otherwise parts of 16 blocks or more, paged_parts of them where the keys suffice, so that the
-// workgroups of short sequences and the ends of long ones fill in.  Measured: 8 x 32
-// heads x 8K keys 160 us, 174 in such finer parts; 8 x 8 heads x 32K 169 and 172; 64 ragged sequences
-// in 8 bits 365 us in finer parts, 474 in as few as the CUs.
+// The quota: units of one size (the longest at most 5/4 of the mean), as many as the CUs or fewer,
+// or nearly twice as many, are cut into as few parts as give every CU one, if those fit at once
+// (paged_slots).  Otherwise parts of 16 blocks or more, paged_parts of them where the keys
+// suffice, so that the workgroups of short sequences and the ends of long ones fill in.  Measured:
+// 8 x 32 heads x 8K keys 160 us, 174 in such finer parts; 16 of them 327 and 326, 15 of them 311
+// and 324, 12 of them 296 and 251, 9 of them 271 and 199; 64 ragged sequences in 8 bits 365 us in
+// finer parts, 474 in as few as the CUs.
 struct PagedSeq {
   int len, n_new, blocks;
 };
@@ -89,34 +90,31 @@ __device__ __forceinline__ int parts_of(int blocks, int quota) {
   return blocks <= quota ? 1 : short_div(blocks - 1, quota) + 1;
 }
 
-// What is common to all parts.
-struct PagedQuota {
-  int quota;
-  bool even;
-};
-// all: the blocks of all units, in fp32, which a quota need not be exact for: an error of 2^-12
+// The quota.  all: the blocks of all units, in fp32, which a quota need not be exact for: an error of 2^-12
 // still leaves the number of parts below what the host has made room for.  most: of the longest.
-__device__ __forceinline__ PagedQuota paged_quota(const PagedAttnArgs& a, float all, int most) {
+__device__ __forceinline__ int paged_quota(const PagedAttnArgs& a, float all, int most) {
   const float seqs = (float)a.c.B * (float)(a.c.Hkv * a.row_blocks);
   auto ceil_of = [](float x) {
     const int c = (int)fminf(x, 1073741824.f);
     return (float)c < x ? c + 1 : c;
   };
   const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
-  const bool even = 0.8f * (float)most * seqs <= all && seqs <= 2.f * kNumCu &&
+  const bool even = 0.8f * (float)most * seqs <= all &&
+                    (seqs <= 1.f * kNumCu || (seqs >= 1.8f * kNumCu && seqs <= 2.f * kNumCu)) &&
                     (float)parts_of(most, fill) * seqs <= a.slots;
-  return {max(1, uniform(even ? fill : max(fine, min(fill, 16)))), even};
+  return max(1, uniform(even ? fill : max(fine, min(fill, 16))));
 }
 // Order: the parts of a whole quota, then the shorter ends, which even out when the
-// workgroups finish.  `whole` of the parts of each of a sequence's units come in the first turn.
+// workgroups finish (7 x 32 heads x 8K keys 156 us; sequence by sequence 232, as CUs got two whole
+// parts).  `whole` of the parts of each of a sequence's units come in the first turn.
 struct PagedCut {
   int parts, whole;
 };
-__device__ __forceinline__ PagedCut paged_cut(const PagedAttnArgs& a, const PagedQuota& q, int b, const PagedSeq& s) {
+__device__ __forceinline__ PagedCut paged_cut(const PagedAttnArgs& a, int quota, int b, const PagedSeq& s) {
   PagedCut c{0, 0};
   if (b < a.c.B) {
-    c.parts = parts_of(s.blocks, q.quota);
-    c.whole = q.even || c.parts * q.quota == s.blocks ? c.parts : c.parts - 1;
+    c.parts = parts_of(s.blocks, quota);
+    c.whole = c.parts * quota == s.blocks ? c.parts : c.parts - 1;
   }
   return c;
 }
@@ -128,9 +126,9 @@ __device__ __forceinline__ int wave_most(int x) {
 }
 
 // The sums that every wave needs to find its part, for batches of more than kPlanBatch sequences,
-// where walking all lengths would cost each wave more than this launch: quota, whether the
-// batch is even, parts of the first turn, 0; then for every 64 sequences the parts of the
-// first turn, and of both, up to their end.  One workgroup.
+// where walking all lengths would cost each wave more than this launch: quota, parts of the first
+// turn; then for every 64 sequences the parts of the first turn, and of both, up to their end.
+// One workgroup.
 template <int BK>
 __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
   __shared__ float sums[16];
@@ -154,9 +152,9 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
     all += sums[w];
     most = max(most, tops[w]);
   }
-  const PagedQuota q = paged_quota(a, all * (float)units, most);
+  const int quota = paged_quota(a, all * (float)units, most);
   for (int i = wave; i < n; i += 16) {
-    const PagedCut c = paged_cut(a, q, 64 * i + lane, paged_seq<BK>(a, 64 * i + lane));
+    const PagedCut c = paged_cut(a, quota, 64 * i + lane, paged_seq<BK>(a, 64 * i + lane));
     const int w = wave_sum(c.whole), x = wave_sum(c.parts);
     if (lane == 0) {
       whole[i] = w;
@@ -179,14 +177,12 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
     x += i < wave ? ends[1][i] : 0;
   }
   if (tid == 0) {
-    a.plan[0] = q.quota;
-    a.plan[1] = q.even;
-    a.plan[2] = first * units;
-    a.plan[3] = 0;
+    a.plan[0] = quota;
+    a.plan[1] = first * units;
   }
   if (tid < n) {
-    a.plan[4 + 2 * tid] = w * units;
-    a.plan[5 + 2 * tid] = x * units;
+    a.plan[2 + 2 * tid] = w * units;
+    a.plan[3 + 2 * tid] = x * units;
   }
 }
 
@@ -226,19 +222,19 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
     r.any = true;
     return r;
   }
-  PagedQuota q;
+  int quota;
   PagedSeq s;
   int first_turn, b0 = 0, before = 0, before_all = 0;   // parts of the turn, and of both, before sequence b0
   bool second;
   if (a.plan) {
-    q = {a.plan[0], a.plan[1] != 0};
-    first_turn = a.plan[2];
+    quota = a.plan[0];
+    first_turn = a.plan[1];
     second = find >= first_turn;
     if (second) find -= first_turn;
     const int n = (p.B + 63) / 64;
     for (int i0 = 0;; i0 += 64) {
       if (i0 >= n) return r;
-      const int i = min(i0 + lane, n - 1), w = a.plan[4 + 2 * i], x = a.plan[5 + 2 * i];
+      const int i = min(i0 + lane, n - 1), w = a.plan[2 + 2 * i], x = a.plan[3 + 2 * i];
       const int own = second ? x - w : w;
       const uint64_t past = __ballot(own > find);
       const int l = past ? __ffsll((unsigned long long)past) - 1 : 64;   // those before end at or below `find`
@@ -261,23 +257,19 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
       all += (float)wave_sum(n);
       most = max(most, wave_most(n));
     }
-    q = paged_quota(a, all * (float)units, most);
-    first_turn = 0x7fffffff;
-    if (!q.even) {
-      first_turn = 0;
-      for (int c0 = 0; c0 < p.B; c0 += 64)
-        first_turn += wave_sum(paged_cut(a, q, c0 + lane, c0 == 0 ? head : paged_seq<BK>(a, c0 + lane)).whole);
-      first_turn *= units;
-    }
+    quota = paged_quota(a, all * (float)units, most);
+    first_turn = 0;
+    for (int c0 = 0; c0 < p.B; c0 += 64)
+      first_turn += wave_sum(paged_cut(a, quota, c0 + lane, c0 == 0 ? head : paged_seq<BK>(a, c0 + lane)).whole);
+    first_turn *= units;
     second = find >= first_turn;
     if (second) find -= first_turn;
   }
-  const int quota = q.quota;
   for (;;) {
-    const PagedCut c = paged_cut(a, q, b0 + lane, s);
+    const PagedCut c = paged_cut(a, quota, b0 + lane, s);
     const int own = (second ? c.parts - c.whole : c.whole) * units;
     const int incl = before + wave_scan(own, 0, add);
-    const int incl_all = q.even ? incl : before_all + wave_scan(c.parts * units, 0, add);
+    const int incl_all = before_all + wave_scan(c.parts * units, 0, add);
     const uint64_t past = __ballot(incl > find);
     if (past) {
       const int l = __ffsll((unsigned long long)past) - 1;

@@ -91,7 +91,7 @@ struct PagedAttnArgs {
   float* o_part;         // [slot][part_rows][D] sums of a workgroup whose keys are a part of its rows'
   float* ml_part;        // [slot][part_rows][2] their maximum (log2 domain) and weight sum
   int32_t* unit;         // [B][H_kv][row_blocks][4]: a unit's first part, parts and rows
-  int32_t* plan;         // nullptr, or 4 + 2 ceil(B / 64) sums of the batch (paged_plan_kernel)
+  int32_t* plan;         // nullptr, or 2 + 2 ceil(B / 64) sums of the batch (paged_plan_kernel)
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
