@@ -331,7 +331,6 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   a.part_rows = plan.part_rows;
   a.max_chunks = plan.max_chunks;
   a.per_part = 1.0f / plan.parts;
-  a.slots = pd::paged_slots((long long)a.c.G * a.c.Ln, a.c.D);
   a.grid = plan.grid;
   a.by_group = pd::fast_div(a.c.G);
   a.by_heads = pd::fast_div(a.c.Hkv);

@@ -57,9 +57,9 @@ struct PagedPart {
 // launch before has left, paged_plan_kernel).
 //
 // The quota: units of one size (the longest at most 5/4 of the mean), as many as the CUs or fewer,
-// or nearly twice as many, are cut into as few parts as give every CU one, if those fit at once
-// (paged_slots).  Otherwise parts of 16 blocks or more, paged_parts of them where the keys
-// suffice, so that the workgroups of short sequences and the ends of long ones fill in.  Measured:
+// or nearly twice as many, are cut into as few parts as give every CU one.  Otherwise parts of 16
+// blocks or more, paged_parts of them where the keys suffice, so that the workgroups of short
+// sequences and the ends of long ones fill in.  Measured:
 // 8 x 32 heads x 8K keys 160 us, 174 in such finer parts; 16 of them 327 and 326, 15 of them 311
 // and 324, 12 of them 296 and 251, 9 of them 271 and 199; 64 ragged sequences in 8 bits 365 us in
 // finer parts, 474 in as few as the CUs.
@@ -100,13 +100,12 @@ __device__ __forceinline__ int paged_quota(const PagedAttnArgs& a, float all, in
   };
   const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
   const bool even = 0.8f * (float)most * seqs <= all &&
-                    (seqs <= 1.f * kNumCu || (seqs >= 1.8f * kNumCu && seqs <= 2.f * kNumCu)) &&
-                    (float)parts_of(most, fill) * seqs <= a.slots;
+                    (seqs <= 1.f * kNumCu || (seqs >= 1.8f * kNumCu && seqs <= 2.f * kNumCu));
   return max(1, uniform(even ? fill : max(fine, min(fill, 16))));
 }
 // Order: the parts of a whole quota, then the shorter ends, which even out when the
-// workgroups finish (7 x 32 heads x 8K keys 156 us; sequence by sequence 232, as CUs got two whole
-// parts).  `whole` of the parts of each of a sequence's units come in the first turn.
+// workgroups finish (7 x 32 heads x 8K keys 156 us, with 32 new rows 174; sequence by sequence 232
+// and 249, as CUs got two whole parts).  `whole` of the parts of each of a sequence's units come in the first turn.
 struct PagedCut {
   int parts, whole;
 };

@@ -95,7 +95,6 @@ struct PagedAttnArgs {
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
-  float slots;           // paged_slots
   long long grid;
   FastDiv by_group, by_heads, by_rows, by_blocks, by_units;  // G, H_kv, G * L_n, row_blocks, H_kv * row_blocks
 };
@@ -106,11 +105,6 @@ struct PagedAttnArgs {
 // 4096), but 4 us for a thousand of those with more than 16 rows, of which it holds one
 // (8 rows of 4 heads over 8 x 8K keys 51.2 us with 1024, 54.1 with 2048, 56.5 with 2900).
 inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
-// Parts that run at once, as far as it matters: up to 16 rows memory bounds the parts of a CU
-// together, but with more rows each part takes its own time, and a second round of them
-// as long again (24 rows of 4 heads over 8 x 8K keys, 192 units in two parts each: 145 us, 99
-// in parts of 16 blocks; 7 x 32 heads, 32 rows 249 and 197).
-inline float paged_slots(long long rows, int d) { return rows <= 16 ? 1e9f : d == 128 ? 256.f : 512.f; }
 // Blocks up to which no unit's keys are cut, and no join follows: 16 where the units alone fill
 // the card (32 ragged sequences of 8 heads, 8 new rows, up to 600 / 2048 keys: cut 26.3 and 44.5 us,
 // whole 16.4 and 36.8; 12 of 32 heads up to 4096 keys, cut 85, whole 95), 4 elsewhere (8 heads

@@ -91,6 +91,16 @@ def test_far_positions(gpu_lib):
     check(fused[:, :2], None, 0, pos, 1e6, qo, PD_FP32)
 
 
+def test_norms_beyond_the_range_of_their_squares(gpu_lib):
+    """2^60 squared times 64 still fits fp32, 2^100 squared does not: zeros."""
+    x = torch.ones(2, 3, 64, device="cuda")
+    x[0] *= 2.0 ** 60
+    x[1] *= 2.0 ** 100
+    w, out = torch.full((64,), 1.5, device="cuda"), torch.full_like(x, 7.0)
+    _lib.pd_qk_norm_rope(x, None, w, None, 1e-6, None, 0.0, out, None)
+    assert torch.all((out[0] - 1.5).abs() <= 1.5 * 4 * 2.0 ** -24) and torch.all(out[1] == 0)   # root, division, two products
+
+
 def test_zero_and_nonfinite_rows(gpu_lib):
     """A row of zeros stays zeros with eps > 0; a non-finite head spoils itself alone."""
     fused, w, pos = rows(6, 4, 2, 64, PD_BF16, 7)
