@@ -295,8 +295,9 @@ def _torch():
     """torch, and the element types by pd_dtype and back, filled in once (loading the library imports it first)."""
     import torch
     if not _TYPES:
-        _TYPES.update({PD_BF16: torch.bfloat16, PD_FP32: torch.float32, PD_FP8_E4M3: torch.float8_e4m3fn})
+        # The table that is asked for above comes last: a thread that finds it filled needs both.
         _KINDS.update({torch.bfloat16: PD_BF16, torch.float32: PD_FP32, "int32": torch.int32, "uint8": torch.uint8})
+        _TYPES.update({PD_BF16: torch.bfloat16, PD_FP32: torch.float32, PD_FP8_E4M3: torch.float8_e4m3fn})
     return torch
 
 

@@ -159,3 +159,19 @@ def test_binding_checks_tensors(lib):
         _lib._rows("x", torch.zeros(2, 5, 6, 64)[:, :4], (2, 4, 6, 64), types, -1)
     with pytest.raises(ValueError, match="contiguous"):
         _lib._checked("x", torch.zeros(6, 4).t(), (4, 6), types, -1)
+
+
+def test_binding_types_are_complete_once_they_are_seen(lib, monkeypatch):
+    """The element types are filled in at the first call; a thread that finds one table filled relies on the other."""
+    kinds = {}
+
+    class Watched(dict):
+        def update(self, *a, **kw):
+            super().update(*a, **kw)
+            assert len(kinds) == 4, "another thread would take the tables for complete here"
+
+    types = Watched()
+    monkeypatch.setattr(_lib, "_KINDS", kinds)
+    monkeypatch.setattr(_lib, "_TYPES", types)
+    _lib._torch()
+    assert len(types) == 3 and set(types.values()) >= {torch.bfloat16, torch.float32}
