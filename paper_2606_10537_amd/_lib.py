@@ -462,6 +462,8 @@ def pd_paged_attn(dims: PagedDims, cache: PagedCache, q, o, lse=None, page_idx=N
     shape, top_k, ip = (B, L, hq, dims.head_dim), 0, None
     if page_idx is not None:
         top_k = page_idx.shape[-1]
+        if top_k < 1:   # a tensor without elements may have no address, which would mean all pages
+            raise ValueError("page_idx has no entries; without a list (None) all pages are attended to")
         ip = _checked("page_idx", page_idx, (B, dims.n_heads_kv, top_k), _KINDS["int32"], dev)
     lp = None if lse is None else _checked("lse", lse, (B, hq, L), _TYPES[PD_FP32], dev)
     _check(load().pd_paged_attn(ctypes.byref(dims), c, _checked("q", q, shape, cache.type, dev), ip, top_k,

@@ -175,3 +175,21 @@ def test_binding_types_are_complete_once_they_are_seen(lib, monkeypatch):
     monkeypatch.setattr(_lib, "_TYPES", types)
     _lib._torch()
     assert len(types) == 3 and set(types.values()) >= {torch.bfloat16, torch.float32}
+
+
+class _OnTheHost:
+    """Stands for a PagedCache, so that the calls' checks run on CPU tensors (whose device number is -1)."""
+    device, type = -1, torch.bfloat16
+
+    def _for(self, dims):
+        return ctypes.byref(cache())
+
+
+def test_an_empty_list_of_pages_is_not_all_pages(lib):
+    """page_idx of no entries has no address, which the library would take for no list at all: refused."""
+    d = dims()
+    q = torch.zeros(2, 1, 8, 128, dtype=torch.bfloat16)
+    idx = torch.zeros(2, 2, 0, dtype=torch.int32)
+    assert idx.data_ptr() == 0
+    with pytest.raises(ValueError, match="page_idx"):
+        _lib.pd_paged_attn(d, _OnTheHost(), q, q.clone(), page_idx=idx)
