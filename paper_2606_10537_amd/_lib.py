@@ -289,6 +289,7 @@ def pd_mfma_rate_probe(n_workgroups, iters, sink, stream=None):
 # and the reason is looked for only where something does not.
 
 _TYPES, _KINDS = {}, {}
+_FAR = 1 << 31
 
 
 def _torch():
@@ -427,6 +428,8 @@ def pd_qk_norm_rope(q, k, w_q, w_k, eps, pos, rope_base, q_out, k_out, stream=No
 
 
 def pd_paged_workspace_bytes(dims: PagedDims, top_k=0, which=1) -> int:
+    if not -_FAR <= top_k < _FAR or not -_FAR <= which < _FAR:   # ctypes would keep the low 32 bits
+        raise ValueError(f"top_k={top_k} and which={which} must fit 32 bits")
     return load().pd_paged_workspace_bytes(ctypes.byref(dims), top_k, which)
 
 
@@ -441,6 +444,8 @@ def pd_paged_append(dims: PagedDims, cache: PagedCache, k_new, v_new, stream=Non
 def pd_paged_read(dims: PagedDims, cache: PagedCache, first, n_rows, k_out, v_out, stream=None):
     """Positions first..first+n_rows-1 of every sequence into k_out, v_out [B, H_kv, n_rows, d] (see include/pd.h)."""
     shape, c, dev = (dims.batch, dims.n_heads_kv, n_rows, dims.head_dim), cache._for(dims), cache.device
+    if not -_FAR <= first < _FAR:
+        raise ValueError(f"first={first} must fit 32 bits")
     _check(load().pd_paged_read(ctypes.byref(dims), c, first, n_rows, _checked("k_out", k_out, shape, cache.type, dev),
                                 _checked("v_out", v_out, shape, cache.type, dev), _launch_stream(stream, dev)))
 
@@ -448,6 +453,8 @@ def pd_paged_read(dims: PagedDims, cache: PagedCache, first, n_rows, k_out, v_ou
 def pd_paged_select(dims: PagedDims, cache: PagedCache, q, top_k, n_first, n_last, page_idx, workspace, stream=None):
     """The top_k pages of each (sequence, KV head) by a bound on their scores (see include/pd.h)."""
     c, dev = cache._for(dims), cache.device
+    if not -_FAR <= n_first < _FAR or not -_FAR <= n_last < _FAR:
+        raise ValueError(f"n_first={n_first} and n_last={n_last} must fit 32 bits")
     qp = _checked("q", q, (dims.batch, dims.new_len, dims.n_heads_q, dims.head_dim), cache.type, dev)
     ip = _checked("page_idx", page_idx, (dims.batch, dims.n_heads_kv, top_k), _KINDS["int32"], dev)
     _check(load().pd_paged_select(ctypes.byref(dims), c, qp, top_k, n_first, n_last, ip, *_space(workspace, dev),

@@ -193,3 +193,20 @@ def test_an_empty_list_of_pages_is_not_all_pages(lib):
     assert idx.data_ptr() == 0
     with pytest.raises(ValueError, match="page_idx"):
         _lib.pd_paged_attn(d, _OnTheHost(), q, q.clone(), page_idx=idx)
+
+
+@pytest.mark.parametrize("far", [1 << 31, 1 << 32, (1 << 32) + 7, -(1 << 32)])
+def test_binding_refuses_numbers_beyond_32_bits(lib, far):
+    """Position and page counts are 32 bits in the library; a larger number is refused, not cut to its low bits."""
+    d = dims()
+    q = torch.zeros(2, 1, 8, 128, dtype=torch.bfloat16)
+    out = torch.zeros(2, 2, 64, 128, dtype=torch.bfloat16)
+    idx = torch.zeros(2, 2, 4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="first"):
+        _lib.pd_paged_read(d, _OnTheHost(), far, 64, out, out.clone())
+    for first, last in ((far, 0), (0, far)):
+        with pytest.raises(ValueError, match="n_first"):
+            _lib.pd_paged_select(d, _OnTheHost(), q, 4, first, last, idx, None)
+    for top_k, which in ((far, 1), (4, far)):
+        with pytest.raises(ValueError, match="top_k"):
+            _lib.pd_paged_workspace_bytes(d, top_k, which)
