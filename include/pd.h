@@ -437,7 +437,8 @@ pd_status pd_paged_select(const pd_paged_dims *dims, const pd_paged_cache *cache
  * NULL.  Rows r >= new_rows[b] of o and lse are left as they were.  A row that
  * sees no position, or only scores of -inf, gets o = 0 and lse = -inf.  What
  * the pages hold behind kv_len is never used, whatever its bits.  A page id
- * outside 0..n_pages-1 that is needed makes the group's rows NaN.
+ * outside 0..n_pages-1 makes the rows of o and lse that see one of its positions NaN,
+ * and no others.
  * The weights are rounded to bf16 before they multiply V with dtype = PD_BF16
  * (their sum, and so lse, is taken before); sums are fp32 and divided at the
  * end, so they overflow where 256 * sum |v| over the visible keys passes 2^128.

@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
   const int sight = p.causal ? len - n_new + 1 + a.by_group.quot(min(rows - 1, row0 + RT * 16 - 1)) : len;
   const int n_steps = (chosen ? part.last : min(part.last, (max(sight, 0) + BK - 1) / BK)) - part.first;
   int at_page[H], at_pos[H];
-  bool bad = false;
+  int bad = kFarPos;                 // the least position on a page outside the pool
   auto locate = [&](int i0) {
     const int i = i0 + lane;
 #pragma unroll
@@ -445,7 +445,7 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
           const int page = table[ord];
           at_pos[h] = pos;
           if ((unsigned)page < (unsigned)p.n_pages) at_page[h] = page;
-          else bad = true;
+          else bad = min(bad, pos);
         }
       }
     }
@@ -718,11 +718,12 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
   }
 
   // Join of the four waves.  Column n of the results is query row n.
-  const bool wave_bad = __any(bad);
+  int spoilt = kFarPos;              // rows that see this position are NaN
+  if (__any(bad < kFarPos)) spoilt = __builtin_amdgcn_readlane(wave_scan(bad, kFarPos, [](int x, int y) { return min(x, y); }), 63);
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
     l[t] = group_sum(l[t]);
-    if (wave_bad) l[t] = NAN;
+    if (spoilt < lim[t]) l[t] = NAN;
     if (g4 == 0) {
       lds_ml[wave][t * 16 + n][0] = m[t];
       lds_ml[wave][t * 16 + n][1] = l[t];

@@ -1,0 +1,58 @@
+"""Where the paged attention's rows part: page ids outside the pool and values that are not finite, which count for the
+rows that see them and for no others, wherever they lie."""
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paged_case import Case, check_attn, run_attn
+from paper_2606_10537_amd._lib import PD_BF16, PD_FP32, PD_FP8_E4M3
+
+pytestmark = pytest.mark.gpu
+KINDS = [(PD_BF16, PD_BF16), (PD_BF16, PD_FP8_E4M3), (PD_FP32, PD_FP32)]
+IDS = ["bf16", "fp8", "fp32"]
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
+@pytest.mark.parametrize("hq,hkv,L,n,bad", [(4, 2, 24, 60, 3),      # 48 rows, two row blocks; the page holds new rows
+                                            (3, 1, 33, 90, 4),      # 99 rows, four row blocks
+                                            (4, 4, 7, 40, 2),       # one block; the page's rows are all new
+                                            (8, 1, 40, 3000, 186),  # 320 rows, keys cut into parts
+                                            (8, 1, 40, 3000, 2)])   # a page that every row sees
+def test_a_bad_page_spoils_the_rows_that_see_it(gpu_lib, dtype, cache, hq, hkv, L, n, bad):
+    """Causal rows: those whose own position lies before the page keep their attention, whatever block of rows they are
+    taken in; without a causal mask all rows see it.  The other sequence is left alone."""
+    R, d = 16, 64
+    for causal in (1, 0):
+        case = Case([n, n], new_len=L, hq=hq, hkv=hkv, d=d, dtype=dtype, cache=cache, R=R, causal=causal, seed=L)
+        c = case.to_gpu()
+        for number in (case.dims.n_pages, -3, (1 << 31) - 1):
+            c["table"][1, bad] = number
+            o, lse = run_attn(case, c)
+            clean = min(L, max(0, bad * R - (n - L))) if causal else 0   # new rows before the page
+            assert torch.isnan(o[1, clean:]).all() and torch.isnan(lse[1, :, clean:]).all()
+            o[1, clean:], lse[1, :, clean:] = 7.0, 7.0
+            part = Case.__new__(Case)
+            part.__dict__.update(case.__dict__, lens=[n, n - L + clean], new=[L, clean])
+            part.held = {k: [v[0], v[1][:n - L + clean]] for k, v in case.held.items()}
+            check_attn(part, o, lse)
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
+def test_a_bad_page_in_a_list(gpu_lib, dtype, cache):
+    """Lists of pages: one that names the bad page is NaN for the rows that see it, one that does not is not."""
+    R, n, L = 16, 64, 20
+    case = Case([n], new_len=L, hq=4, hkv=2, d=64, dtype=dtype, cache=cache, R=R, seed=3)
+    c = case.to_gpu()
+    c["table"][0, 3] = case.dims.n_pages + 5                          # positions 48..63: new rows 4..19
+    idx = torch.tensor([[[3, 0, 1], [0, 2, -1]]], dtype=torch.int32, device="cuda")
+    o, lse = run_attn(case, c, page_idx=idx)
+    assert torch.isnan(o[0, 4:, :2]).all() and torch.isnan(lse[0, :2, 4:]).all()
+    assert torch.isfinite(o[0, :4, :2]).all() and torch.isfinite(o[0, :, 2:]).all() and torch.isfinite(lse[0, 2:]).all()
+    part = Case.__new__(Case)
+    part.__dict__.update(case.__dict__, lens=[n - L + 4], new=[4])
+    part.held = {k: [v[0][:n - L + 4]] for k, v in case.held.items()}
+    o[:, 4:], lse[:, :, 4:] = 7.0, 7.0
+    check_attn(part, o, lse, page_idx=idx.cpu())
