@@ -442,6 +442,8 @@ pd_status pd_paged_select(const pd_paged_dims *dims, const pd_paged_cache *cache
  * The weights are rounded to bf16 before they multiply V with dtype = PD_BF16
  * (their sum, and so lse, is taken before); sums are fp32 and divided at the
  * end, so they overflow where 256 * sum |v| over the visible keys passes 2^128.
+ * A visible value that is infinite gives the infinity, or NaN where its weight
+ * has underflowed (about 2^-126 of the row's largest); NaN gives NaN.
  * The lengths are known on the device alone: the split of long sequences over
  * workgroups, and their join, are planned there.
  * Exponent bytes are those that pd_paged_append writes.

@@ -364,9 +364,10 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 
 // STREAM: the keys are read by one workgroup alone (non-temporal loads: 8 x 32 heads x 32K keys 648
 // against 723 us, 64 ragged sequences in 8 bits 381 against 402); row blocks that share them leave
-// them in the caches.
+// them in the caches.  Waves a SIMD: what the registers of each form leave room for (two blocks of 16
+// rows in d = 64 use 168 in 8 bits, and more would cost the third wave).
 template <int D, int CT, int RT, bool STREAM>
-__global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
@@ -661,16 +662,22 @@ __global__ __launch_bounds__(256, D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) v
       }
       if (!whole && any_odd) {
         for (int key = 0; key < S::KS; ++key) {
+          // The row's weight of the key, from the lane that holds it: a value counts with its weight
+          // as in a product, so where this has underflowed an infinity gives NaN here too.
+          float w = pr[0][0];
+#pragma unroll
+          for (int i = 1; i < 4 * H; ++i) w = (key >> 4) * 4 + key % 4 == i ? pr[i / 4][i % 4] : w;
+          w = __shfl(w, 16 * (key / 4 % 4) + n);
           if ((key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16 >= lim[t]) continue;
-          const float* copy = &lds_o[wave][0][0] + key * (CT == kFp32 ? D : D / 2);
+          const uint32_t* copy = (const uint32_t*)&lds_o[wave][0][0] + key * (CT == kFp32 ? D : D / 2);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
               const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : S::base(4 * g4 + r) + i;
-              const uint32_t u = __float_as_uint(copy[CT == kFp32 ? ch : ch / 2]);
+              const uint32_t u = copy[CT == kFp32 ? ch : ch / 2];
               const float x = __uint_as_float(CT == kFp32 ? u : i & 1 ? u & 0xffff0000u : u << 16);
-              if (!(fabsf(x) < INFINITY)) o[t][i][r] += x;
+              if (!(fabsf(x) < INFINITY)) o[t][i][r] += w * x;
             }
         }
       }

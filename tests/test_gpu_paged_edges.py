@@ -56,3 +56,49 @@ def test_a_bad_page_in_a_list(gpu_lib, dtype, cache):
     part.held = {k: [v[0][:n - L + 4]] for k, v in case.held.items()}
     o[:, 4:], lse[:, :, 4:] = 7.0, 7.0
     check_attn(part, o, lse, page_idx=idx.cpu())
+
+
+@pytest.mark.parametrize("dtype", [PD_BF16, PD_FP32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_infinite_values_count_with_their_weight_wherever_they_lie(gpu_lib, dtype, d):
+    """An infinite value whose weight is there gives its infinity; one whose weight has underflowed (e^-400 of the
+    largest) gives 0 * inf = NaN: among whole steps, in the last keys of a single row, and at positions that some of
+    several causal rows see.  Other channels and rows are finite, whatever the place."""
+    n = 700
+    for L, at in ((1, 40), (1, n - 1), (1, n - 20), (4, 40), (4, n - 4), (4, n - 3), (40, n - 38), (40, 300)):
+        for score, top in ((400.0, 17), (400.0, at - 5), (0.0, 17)):  # of one key above all others, the infinite one's too
+            for bad in (math.inf, -math.inf):
+                case = Case([n], new_len=L, hq=2, hkv=2, d=d, dtype=dtype, R=32, seed=L)
+                for x in (case.q, *case.k_rows):
+                    x.zero_()
+                case.q[:, :, :, 0] = 160.0 * math.sqrt(d / 64)        # score = q_0 k_0 / sqrt(d)
+                case.k_rows[0][top, :, 0] = score / 20
+                case.v_rows[0][at, 0, 5] = bad
+                case.place()
+                o, lse = run_attn(case, case.to_gpu())
+                first = max(0, at - (n - L))                          # the first new row that sees it
+                hit = o[0, first:, 0, 5].float()
+                assert torch.isnan(hit).all() if score else (hit == bad).all(), (L, at, score, bad, hit)
+                o[0, first:, 0, 5] = 0.0
+                assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("dtype,cache", KINDS, ids=IDS)
+def test_nan_values_spoil_their_channel_alone(gpu_lib, dtype, cache):
+    """A NaN value, however small its weight, in whole and in masked steps.  In 8 bits too: the row's other channels
+    keep their values."""
+    n = 700
+    for L, at in ((1, 40), (1, n - 1), (4, 40), (4, n - 3), (40, n - 38)):
+        for score, top in ((400.0, 17), (400.0, at - 5), (0.0, 17)):
+            case = Case([n], new_len=L, hq=2, hkv=2, d=64, dtype=dtype, cache=cache, R=32, seed=L)
+            for x in (case.q, *case.k_rows):
+                x.zero_()
+            case.q[:, :, :, 0] = 160.0
+            case.k_rows[0][top, :, 0] = score / 20
+            case.v_rows[0][at, 0, 5] = math.nan
+            case.place()
+            o, lse = run_attn(case, case.to_gpu())
+            first = max(0, at - (n - L))
+            assert torch.isnan(o[0, first:, 0, 5]).all()
+            o[0, first:, 0, 5] = 0.0
+            assert torch.isfinite(o).all() and torch.isfinite(lse).all()
