@@ -648,15 +648,34 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           for (int i = 0; i < NT; ++i)
             o[t][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j][i]), pr[0][j], o[t][i], 0, 0, 0);
       } else {
-        // The weights are rounded to bf16 here, to nearest; their sum l is taken before.
-        const u32x4 pw = {pack_bf16x2(pr[0][0], pr[0][1]), pack_bf16x2(pr[0][2], pr[0][3]),
-                          pack_bf16x2(pr[H - 1][0], pr[H - 1][1]), pack_bf16x2(pr[H - 1][2], pr[H - 1][3])};
+        // The weights as bf16; their sum l is taken before.  One tile of rows: two terms, the upper half of
+        // the weight's bits and the rest rounded, 15 bits or more, so that the output's rounding is what is left
+        // of the error (64 ragged requests in 8 bits 1.95e-3 of the 2-norm with weights of one term, 1.65e-3 with two);
+        // memory bounds such calls, and the second product costs nothing there (8 x 32 heads x 32K keys 614.5 and
+        // 615.1 us, one token of 8K keys 10.2 and 10.3).  Two tiles: one term, rounded to nearest; the second would be
+        // paid for (32 rows of 4 heads over 8 x 8K keys 85.4 us with one, 89.1 with two; in 8 bits 84.4 and 97.9, d = 64
+        // 50.3 and 57.4).
+        u32x4 pw, pl;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = pr[j < 2 ? 0 : H - 1][2 * (j & 1)], y = pr[j < 2 ? 0 : H - 1][2 * (j & 1) + 1];
+          if constexpr (RT == 1) {
+            const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+            pw[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            // 2^-24 of the weight more: a second term of zero would turn infinite values into NaN
+            pl[j] = pack_bf16x2(fmaf(x, 0x1p-24f, x - __uint_as_float(a & 0xffff0000u)),
+                                fmaf(y, 0x1p-24f, y - __uint_as_float(b & 0xffff0000u)));
+          } else {
+            pw[j] = pack_bf16x2(x, y);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
           u32x4 w;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             w[j] = __builtin_amdgcn_perm(v[2 * j + 1][i / 2], v[2 * j][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
+          if constexpr (RT == 1) o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pl), o[t][i]);
           o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), o[t][i]);
         }
       }

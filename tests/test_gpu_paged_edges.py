@@ -7,7 +7,8 @@ import numpy as np
 import pytest
 import torch
 
-from paged_case import Case, check_attn, run_attn
+import oracle.paged as ref
+from paged_case import HALF_STEP, Case, check_attn, h64, run_attn
 from paper_2606_10537_amd._lib import PD_BF16, PD_FP32, PD_FP8_E4M3
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +103,22 @@ def test_nan_values_spoil_their_channel_alone(gpu_lib, dtype, cache):
             assert torch.isnan(o[0, first:, 0, 5]).all()
             o[0, first:, 0, 5] = 0.0
             assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("cache", [PD_BF16, PD_FP8_E4M3], ids=["bf16", "fp8"])
+@pytest.mark.parametrize("hq,hkv,L,lens,d", [(4, 4, 1, [3, 40, 300], 64), (28, 4, 1, [700, 33, 2], 128), (16, 1, 1, [5000, 129], 128),
+                                             (4, 2, 8, [90, 2000], 64), (2, 2, 16, [16, 260], 128)])
+def test_weights_of_sixteen_bits(gpu_lib, cache, hq, hkv, L, lens, d):
+    """Up to 16 query rows a KV head the weights multiply V as two bf16 terms: the first cut off (the second is below
+    2^-7 of the weight), the second rounded (2^-8 of itself): 2^-15 of the weight together.  The rest as in check_attn."""
+    case = Case(lens, new_len=L, hq=hq, hkv=hkv, d=d, cache=cache, R=32, seed=hq + L)
+    o, lse = run_attn(case, case.to_gpu())
+    check_attn(case, o, lse)
+    G = hq // hkv
+    for b in range(len(lens)):
+        for g in range(hkv):
+            k, v = case.held["k"][b][:, g], case.held["v"][b][:, g]
+            want, _, mass, spread = ref.attn_ref(case.rows_of(b, g), k, v, case.ends(b), case.scale)
+            delta = (2 * (d + 4) * 2.0 ** -24 * spread + 2.0 ** -21 + len(k) * 2.0 ** -24)[:, None]
+            err = np.abs(h64(o[b, :, g * G:(g + 1) * G]).reshape(-1, d) - want)
+            assert np.all(err <= mass * (2 * delta + 2.0 ** -15) + np.abs(want) * HALF_STEP[PD_BF16] + 1e-37)
