@@ -118,3 +118,18 @@ def test_zero_and_nonfinite_rows(gpu_lib):
     same = torch.ones(6, 6, dtype=torch.bool)
     same[1, 2] = same[3, 0] = same[4, 5] = False
     assert torch.equal(a[same], b[same])
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_sines_and_cosines_keep_their_leading_bits_near_zero(gpu_lib, d):
+    """Rows (1, .., 1, 0, .., 0) turn into the cosines and sines themselves.  Each is good to two units in the last place
+    (2 * 2^-23 of itself) and three roundings, at the angle itself, not at the nearest fp32 one: the angle in double
+    is off by at most 8 * 2^-53 of 131072 / 2 pi turns, 2^-33 rad, and so is the oracle's."""
+    T = 4096
+    pos = (torch.arange(T, dtype=torch.int32, device="cuda") * 32 + 7)
+    x = torch.cat([torch.ones(T, 1, d // 2, device="cuda"), torch.zeros(T, 1, d // 2, device="cuda")], -1)
+    out = torch.empty_like(x)
+    _lib.pd_qk_norm_rope(x, None, None, None, 0.0, pos, 5e5, out, None)
+    want = ref.qk_norm_rope_ref(h64(x), None, 0, h64(pos), 5e5)
+    err = np.abs(h64(out) - want)
+    assert np.all(err <= (2 * 2.0 ** -23 + 3 * 2.0 ** -24) * np.abs(want) + 2.0 ** -32), err.max()
