@@ -411,10 +411,13 @@ pd_status pd_paged_read(const pd_paged_dims *dims, const pd_paged_cache *cache, 
  * Chooses pages for each query: for sequence b and KV head g, a page's score is
  * the largest, over the G * new_rows[b] query rows of the group (G = H_q/H_kv),
  * of  sum_i q_i * (q_i >= 0 ? hi_i : lo_i)  with the page's bounds lo, hi: no
- * key of the page has a larger product with the row.  Products and sums are in
- * double precision.  The top_k best of the sequence's ceil(kv_len/R) pages are
- * kept; its first n_first and last n_last pages rank above all others, a NaN score above every
- * number, and ties go to the lower page.
+ * key of the page, as it was given to pd_paged_append, has a larger product with the
+ * row.  The keys that an E4M3 cache holds of them are rounded, by at most 2^-4 of an
+ * element, 2^-17 of the row's largest or 2^-110, so their products may exceed the
+ * score by as much.  Products and sums are in double precision.  The top_k best of
+ * the sequence's ceil(kv_len/R) pages are kept; its first n_first and last n_last
+ * pages rank above all others, a NaN score above every number, and ties go to the
+ * lower page.
  * q [B][L_n][H_q][d] (dtype).  page_idx int32 [B][H_kv][top_k]: the kept pages'
  * indices in the sequence (p / R), ascending; -1 behind the last where the
  * sequence has fewer pages.

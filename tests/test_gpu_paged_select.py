@@ -119,3 +119,41 @@ def test_page_lists_of_the_callers(gpu_lib):
     two, l2 = run_attn(case, c, page_idx=torch.tensor([[[2, 2]], [[2, 2]]], dtype=torch.int32).cuda())
     np.testing.assert_allclose(h64(l2), h64(l1) + math.log(2), atol=1e-5)
     np.testing.assert_allclose(h64(two), h64(one), rtol=2.0 ** -7, atol=2.0 ** -7)
+
+
+@pytest.mark.parametrize("dtype,cache", [(PD_BF16, PD_BF16), (PD_BF16, PD_FP8_E4M3), (PD_FP32, PD_FP32)], ids=["bf16", "fp8", "fp32"])
+def test_the_bound_holds_for_the_keys_of_a_page(gpu_lib, dtype, cache):
+    """Bounds and rows as pd_paged_append writes them.  No given key has a larger product with a query than its page's
+    score; a key that the pages hold exceeds it by its rounding to E4M3 at most, and can (a key of 1.9375 is held as
+    2, one of -1.9375 as -2)."""
+    n, R, d = 150, 32, 64
+    case = Case([n], new_len=n, hq=4, hkv=2, d=d, dtype=dtype, cache=cache, R=R, seed=11)
+    case.k_rows[0][70:90] = 1.9375 * torch.sign(case.k_rows[0][70:90])
+    c = case.to_gpu()
+    k = case.k_rows[0][None].cuda()
+    _lib.pd_paged_append(case.dims, c["cache"], k, k)
+    held = [torch.empty(1, 2, n, d, dtype=case.q.dtype, device="cuda") for _ in range(2)]
+    _lib.pd_paged_read(case.dims, c["cache"], 0, n, *held)
+    bounds, q, given, held = h64(c["bounds"]), h64(case.q[0]), h64(case.k_rows[0]), h64(held[0][0])
+    beyond = 0
+    for g in range(2):
+        rows = q[:, 2 * g:2 * g + 2].reshape(-1, d)
+        for j in range(-(-n // R)):
+            lo, hi = bounds[int(case.table[0, j]), g]
+            score = np.where(rows >= 0, rows * hi, rows * lo).sum(-1)[:, None]
+            x, y = given[j * R:(j + 1) * R, g], held[g, j * R:(j + 1) * R]
+            tiny = 1e-12 * (np.abs(rows) @ np.abs(x).T)                 # this test's own sums in double
+            assert np.all(rows @ x.T <= score + tiny)
+            off = np.abs(rows) @ (2.0 ** -4 * np.abs(x) + 2.0 ** -17 * np.abs(x).max(-1, keepdims=True) + 2.0 ** -110).T
+            assert np.all(rows @ y.T <= score + tiny + (off if cache == PD_FP8_E4M3 else 0))
+            beyond += int((rows @ y.T > score + tiny).sum())
+    assert beyond == 0 or cache == PD_FP8_E4M3
+    ones = np.ones(d)                                                   # one row of equal keys: its page's score is its product
+    case = Case([1], hq=1, hkv=1, d=d, dtype=dtype, cache=cache, R=16, seed=1)
+    c = case.to_gpu()
+    k = torch.full((1, 1, 1, d), 1.9375, dtype=case.q.dtype, device="cuda")
+    _lib.pd_paged_append(case.dims, c["cache"], k, k)
+    held = [torch.empty(1, 1, 1, d, dtype=case.q.dtype, device="cuda") for _ in range(2)]
+    _lib.pd_paged_read(case.dims, c["cache"], 0, 1, *held)
+    score = (ones * h64(c["bounds"])[int(case.table[0, 0]), 0, 1]).sum()
+    assert score == 1.9375 * d and ones @ h64(held[0][0, 0, 0]) == (2.0 if cache == PD_FP8_E4M3 else 1.9375) * d
