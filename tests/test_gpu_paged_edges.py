@@ -122,3 +122,30 @@ def test_weights_of_sixteen_bits(gpu_lib, cache, hq, hkv, L, lens, d):
             delta = (2 * (d + 4) * 2.0 ** -24 * spread + 2.0 ** -21 + len(k) * 2.0 ** -24)[:, None]
             err = np.abs(h64(o[b, :, g * G:(g + 1) * G]).reshape(-1, d) - want)
             assert np.all(err <= mass * (2 * delta + 2.0 ** -15) + np.abs(want) * HALF_STEP[PD_BF16] + 1e-37)
+
+
+@pytest.mark.parametrize("dtype", [PD_BF16, PD_FP32])
+def test_infinite_keys(gpu_lib, dtype):
+    """A key with an infinite element: where the score is -inf the key is as if it were not there, where it is +inf the row
+    is NaN (inf - inf).  In whole steps and at a new row's position, which the rows before do not see."""
+    seen = []
+    for L, n, at in ((6, 50, 47), (1, 700, 20), (6, 700, 20), (40, 700, 690)):
+        for bad in (math.inf, -math.inf):
+            case = Case([n], new_len=L, hq=8, hkv=2, d=128, dtype=dtype, R=16, seed=12)
+            case.k_rows[0][at, 0, 3] = bad
+            case.place()
+            o, lse = run_attn(case, case.to_gpu())
+            for g in range(2):
+                keep = np.arange(n) != (at if g == 0 else n)
+                q, k, v = case.rows_of(0, g), case.held["k"][0][keep, g], case.held["v"][0][keep, g]
+                want, l, mass, spread = ref.attn_ref(q, k, v, case.ends(0), case.scale, np.arange(n)[keep])
+                delta = (2 * (128 + 4) * 2.0 ** -24 * spread + 2.0 ** -21 + n * 2.0 ** -24)[:, None]
+                tol = mass * (2 * delta + (2.0 ** -8 if dtype == PD_BF16 else 0)) + np.abs(want) * HALF_STEP[dtype] + 1e-37
+                got, gl = h64(o[0, :, 4 * g:4 * g + 4]).reshape(-1, 128), h64(lse[0, 4 * g:4 * g + 4]).T.reshape(-1)
+                above = (case.ends(0) > at) & (q[:, 3] * bad > 0) & (g == 0)
+                seen += [above.sum(), ((case.ends(0) > at) & ~above).sum()] if g == 0 else []
+                assert np.all(np.isnan(got[above])) and np.all(np.isnan(gl[above]))
+                rest = ~above
+                assert np.all(np.abs(got - want)[rest] <= tol[rest])
+                assert np.all(np.abs(gl - l)[rest] <= (delta[:, 0] + 2.0 ** -21 * (1 + np.abs(l)))[rest])
+    assert sum(seen[::2]) > 20 and sum(seen[1::2]) > 20               # rows with scores of +inf, and of -inf
