@@ -290,3 +290,48 @@ def test_grids_beyond_one_dimension(gpu_lib):
     out = [torch.empty(B, H, 2, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
     _lib.pd_paged_read(dims, cache, 1, 2, *out)
     assert torch.equal(out[0], out[0][:1].expand_as(out[0])) and torch.equal(out[0][0], k[0, :, 1:3])
+
+
+def test_streams_over_spoilt_caches(gpu_lib):
+    """Three layers at once on streams of their own, over pages, bounds, lists and workspaces that hold nothing but NaN,
+    255 and -1 before: a call that ran ahead of the one whose results it reads would show it."""
+    def fresh():
+        out = []
+        for i in range(3):
+            y = Layer([500 + 100 * i, 33], 900, hq=4, hkv=2, d=128, top_k=5, seed=i)
+            for t in (y.k, y.v, *y.cache.tensors[2:4]):
+                t.view(torch.uint8).fill_(255)
+            y.bounds.fill_(math.nan)
+            y.idx.fill_(-1)
+            for w in y.ws:
+                w.fill_(255)
+            L = max(y.prompts)
+            out.append((y, y.projected(L).cuda(), torch.arange(L, dtype=torch.int32).repeat(y.B).cuda(), L,
+                        [y.projected(1).cuda() for _ in range(4)]))
+        torch.cuda.synchronize()
+        return out
+
+    def go(y, x, pos, L, tokens, stream):
+        y.kv_len.copy_(torch.tensor(y.prompts, dtype=torch.int32, device="cuda"))
+        y.new_rows.copy_(y.kv_len)
+        outs = [y.step(x, pos, L, stream)[2:]]
+        y.new_rows.fill_(1)
+        for tok in tokens:
+            y.kv_len.add_(1)
+            outs.append((*y.step(tok, y.kv_len - 1, 1, stream)[2:], y.idx.clone()))
+        return outs
+
+    want = []
+    for w in fresh():
+        want.append(go(*w, torch.cuda.current_stream()))
+        torch.cuda.synchronize()
+    got, layers, streams = [], fresh(), [torch.cuda.Stream() for _ in range(3)]
+    for w, s in zip(layers, streams):
+        with torch.cuda.stream(s):
+            got.append(go(*w, s))
+    torch.cuda.synchronize()
+    for layer in zip(got, want):
+        for step in zip(*layer):
+            for a, b in zip(*step):
+                assert torch.equal(a, b)
+    assert all(torch.isfinite(t).all() for outs in want for step in outs for t in step[:1])
