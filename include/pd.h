@@ -313,7 +313,9 @@ pd_status pd_gather_joint(const pd_dims *dims, int32_t top_k, int32_t tok_budget
  *   out_i = y_i cos a - y_{i+d/2} sin a,  out_{i+d/2} = y_{i+d/2} cos a + y_i sin a.
  * w_q (w_k) NULL: the query (key) heads are not normalised.  rope_base = 0: no
  * rotation, pos may be NULL.  Norms in fp32 (a head whose squares sum to more
- * than fp32 holds gives zeros); the angle in double precision,
+ * than fp32 holds gives zeros; with eps = 0 the mean square has to be at least 2^-126,
+ * one that vanishes in fp32 gives infinities, and NaN for elements of zero); the
+ * angle in double precision,
  * reduced to one turn before its sine and cosine are taken in fp32; one
  * rounding to the element type at the end.
  *

@@ -133,3 +133,17 @@ def test_sines_and_cosines_keep_their_leading_bits_near_zero(gpu_lib, d):
     want = ref.qk_norm_rope_ref(h64(x), None, 0, h64(pos), 5e5)
     err = np.abs(h64(out) - want)
     assert np.all(err <= (2 * 2.0 ** -23 + 3 * 2.0 ** -24) * np.abs(want) + 2.0 ** -32), err.max()
+
+
+def test_norms_without_eps_at_the_lower_end_of_their_squares(gpu_lib):
+    """eps = 0: a mean square of 2^-126 is still there, one that vanishes in fp32 divides by zero."""
+    x = torch.ones(3, 1, 64, device="cuda")
+    x[0] *= 2.0 ** -63
+    x[1] *= 2.0 ** -80
+    x[2] = 0
+    w, out = torch.full((64,), 1.5, device="cuda"), torch.full_like(x, 7.0)
+    _lib.pd_qk_norm_rope(x, None, w, None, 0.0, None, 0.0, out, None)
+    assert torch.all((out[0] - 1.5).abs() <= 1.5 * 4 * 2.0 ** -24)        # root, division, two products
+    assert torch.all(torch.isinf(out[1])) and torch.all(torch.isnan(out[2]))
+    _lib.pd_qk_norm_rope(x, None, w, None, 1e-12, None, 0.0, out, None)   # with eps all are finite
+    assert torch.isfinite(out).all() and torch.all(out[2] == 0)
