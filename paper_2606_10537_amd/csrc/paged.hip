@@ -23,8 +23,8 @@ namespace pd {
 // and hand the sines and cosines over through LDS.
 //
 // U: head groups a wave loads before it uses the first.  STREAM: loads and stores past the
-// caches, for calls beyond what these hold (32768 rows of 64 heads 191 us, 210 without; a 4096-row
-// call of 40 heads 20.4 and 21.0, and there the reader finds the rows in the caches).
+// caches, for calls beyond what these hold (32768 rows of 64 heads 178 us, 197 without; a 4096-row
+// call of 40 heads 17.3 and 18.2, and there the reader finds the rows in the caches).
 template <bool BF16, int D, int U, bool STREAM>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(NormRopeArgs a) {
   constexpr int E = BF16 ? 8 : 4;       // elements of a lane

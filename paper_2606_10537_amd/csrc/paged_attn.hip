@@ -14,8 +14,9 @@
 //   evenly; rows whose keys are cut are joined by a second kernel.
 //
 // Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
-// nothing but read reaches 6.5 to 7.1 here); in 8 bits 335 us, 6.4 TB/s; 64 ragged sequences of up to
-// 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s.  One token of one 8K sequence takes 7.2 +
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; 64 ragged sequences of up to
+// 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s (its loads bound it: 368 us with the arithmetic
+// of the whole steps left out, 215 with their loads left out).  One token of one 8K sequence takes 7.2 +
 // 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
 // every CU has one.
 //
