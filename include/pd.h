@@ -58,8 +58,8 @@ typedef enum {
   PD_ERR_HIP = 6          /* a kernel launch failed                               */
 } pd_status;
 
-/* PD_FP8_E4M3: the elements of a paged cache only (see pd_paged_dims). */
-typedef enum { PD_BF16 = 0, PD_FP32 = 1, PD_FP8_E4M3 = 2 } pd_dtype;
+/* PD_FP8_E4M3, PD_FP4_E2M1: the elements of a paged cache only (see pd_paged_dims). */
+typedef enum { PD_BF16 = 0, PD_FP32 = 1, PD_FP8_E4M3 = 2, PD_FP4_E2M1 = 3 } pd_dtype;
 
 typedef struct {
   int32_t batch;        /* B >= 1                                                   */
@@ -350,6 +350,14 @@ pd_status pd_qk_norm_rope(int32_t n_rows, int32_t n_heads_q, int32_t n_heads_kv,
  * x * 2^-e rounded to nearest even, and the byte e + 127 is kept beside them.
  * NaN and infinities become NaN.  Scaling by a power of two is exact, so that
  * the rounding to E4M3 is the only one.
+ *
+ * With cache_dtype = PD_FP4_E2M1 a head's row is held as E2M1 values (0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives, codes 0..7 and 8..15 in this order), two a
+ * byte with the even channel in the low four bits, times a power of two for each
+ * 32 neighbouring channels: e is the least exponent with max|x| <= 6 * 2^e over
+ * them, within -100..126 (-100 for zeros), the values are x * 2^-e rounded to
+ * nearest even, and the byte e + 127 is kept.  Where one of the 32 is NaN or an
+ * infinity the byte is 255, and all of them read as NaN.
  */
 typedef struct {
   int32_t batch;        /* B, 1..65536 sequences                                    */
@@ -358,7 +366,8 @@ typedef struct {
   int32_t n_heads_kv;   /* H_kv >= 1, divides H_q                                    */
   int32_t head_dim;     /* d, 64 or 128                                              */
   int32_t dtype;        /* of queries, new rows and outputs: PD_BF16 or PD_FP32      */
-  int32_t cache_dtype;  /* of the pages: dtype, or PD_FP8_E4M3 when dtype = PD_BF16  */
+  int32_t cache_dtype;  /* of the pages: dtype, or PD_FP8_E4M3 or PD_FP4_E2M1 when
+                           dtype = PD_BF16                                           */
   int32_t page_rows;    /* R: 16, 32, 64, 128 or 256                                 */
   int32_t n_pages;      /* pages in the pool, >= 1                                   */
   int32_t max_pages;    /* entries of a sequence in page_table, >= 1                 */
@@ -370,9 +379,10 @@ typedef struct {
 /* Device memory of the cache.  kv_len and new_rows are read on the device:
  * values outside 0..max_pages*R and 0..L_n are taken as the nearer bound. */
 typedef struct {
-  void *k_pages, *v_pages;    /* [n_pages][H_kv][R][d], cache_dtype                  */
-  uint8_t *k_exp, *v_exp;     /* [n_pages][H_kv][R] exponent bytes; PD_FP8_E4M3 only,
-                                 else NULL                                           */
+  void *k_pages, *v_pages;    /* [n_pages][H_kv][R][d], cache_dtype (PD_FP4_E2M1:
+                                 [n_pages][H_kv][R][d/2] bytes)                      */
+  uint8_t *k_exp, *v_exp;     /* exponent bytes: PD_FP8_E4M3 [n_pages][H_kv][R],
+                                 PD_FP4_E2M1 [n_pages][H_kv][d/32][R], else NULL     */
   void *k_bounds;             /* [n_pages][H_kv][2][d], dtype: per channel the least
                                  and the largest key of a page, as given to
                                  pd_paged_append (before quantisation); NULL: not
@@ -402,8 +412,9 @@ pd_status pd_paged_append(const pd_paged_dims *dims, const pd_paged_cache *cache
  * first..first+n_rows-1 of every sequence, dequantised; this is the prefix
  * layout of pd_sparse_decode_attn_compact.  Rows of positions >= kv_len[b] are
  * left as they were.  A page id outside 0..n_pages-1 gives NaN rows.  What an
- * E4M3 value times its power of two stands for is exact in bf16, except that
- * 2^128, which magnitudes from 1.9375 * 2^127 round to, reads as infinity.
+ * E4M3 or E2M1 value times its power of two stands for is exact in bf16, except that
+ * 2^128, which magnitudes from 1.9375 * 2^127 (E2M1: 1.75 * 2^127) round to, reads as
+ * infinity.
  * Sizes: first >= 0, n_rows >= 1, first + n_rows <= max_pages * R.  No workspace.
  */
 pd_status pd_paged_read(const pd_paged_dims *dims, const pd_paged_cache *cache, int32_t first, int32_t n_rows,

@@ -58,6 +58,41 @@ def quantise_ref(x):
     return e4m3_round(y), e
 
 
+# The values of the codes 0..7 of E2M1; 8..15 are their negatives.
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def e2m1_codes(x):
+    """x (|x| <= 6) to the code of the nearest E2M1 value, ties to the even code."""
+    x = np.asarray(x, np.float64)
+    a = np.abs(x)[..., None]
+    off = np.abs(a - E2M1)
+    code = np.argmin(off + 1e-9 * (np.arange(8) % 2), -1)     # neighbours are equally far at a border, and one is even
+    return code + 8 * np.signbit(x)
+
+
+def quantise4_ref(x):
+    """Rows [..., d] to (codes [..., d], exponents [..., d / 32]): e least with max|x| <= 6 * 2^e over 32 channels; a group
+    with an element that is not finite has exponent 128 (its byte is 255)."""
+    x = np.asarray(x, np.float64)
+    x = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
+    bad = ~np.isfinite(x).all(-1)
+    x = np.where(np.isfinite(x), x, 0)
+    a = np.abs(x).max(-1)
+    e = np.full(a.shape, -100)
+    while np.any(short := (e < 126) & (a > 6.0 * 2.0 ** e.astype(np.float64))):
+        e[short] += 1
+    codes = e2m1_codes(x * 2.0 ** -e[..., None].astype(np.float64))
+    return codes.reshape(*codes.shape[:-2], 32 * codes.shape[-2]), np.where(bad, 128, e)
+
+
+def held4_ref(codes, e):
+    """What codes and exponents of quantise4_ref stand for."""
+    v = E2M1[codes % 8] * np.where(codes >= 8, -1.0, 1.0)
+    scale = np.where(e == 128, np.nan, 2.0 ** np.minimum(e, 127).astype(np.float64))
+    return v * np.repeat(scale, 32, -1)
+
+
 def page_scores_ref(q, lo, hi):
     """q [rows, d], lo, hi [pages, d] -> [pages]: the largest over the rows of the bound on q . key."""
     q = np.asarray(q, np.float64)[:, None]

@@ -13,7 +13,7 @@ from dataclasses import dataclass
 PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(PKG, "libpd.so")
 
-PD_BF16, PD_FP32, PD_FP8_E4M3 = 0, 1, 2
+PD_BF16, PD_FP32, PD_FP8_E4M3, PD_FP4_E2M1 = 0, 1, 2, 3
 STATUS = {0: "PD_OK", 1: "PD_ERR_NULL_PTR", 2: "PD_ERR_BAD_DIMS", 3: "PD_ERR_UNSUPPORTED",
           4: "PD_ERR_MISALIGNED", 5: "PD_ERR_WORKSPACE", 6: "PD_ERR_HIP"}
 
@@ -364,8 +364,9 @@ class PagedCache:
     """The tensors of a paged cache (see pd_paged_cache in include/pd.h), checked against `dims` once and kept alive.
 
     k_pages, v_pages [n_pages][H_kv][R][d]; page_table int32 [B][max_pages]; kv_len, new_rows int32 [B]; k_exp, v_exp
-    uint8 [n_pages][H_kv][R] for PD_FP8_E4M3; k_bounds [n_pages][H_kv][2][d].  Calls may bring dims of their own that
-    differ in new_len, n_heads_q, sm_scale and causal."""
+    uint8 [n_pages][H_kv][R] for PD_FP8_E4M3; k_bounds [n_pages][H_kv][2][d].  PD_FP4_E2M1: k_pages, v_pages uint8
+    [n_pages][H_kv][R][d/2], k_exp, v_exp uint8 [n_pages][H_kv][d/32][R].  Calls may bring dims of their own that differ in
+    new_len, n_heads_q, sm_scale and causal."""
 
     def __init__(self, dims, k_pages, v_pages, page_table, kv_len, new_rows=None, k_exp=None, v_exp=None,
                  k_bounds=None):
@@ -373,18 +374,22 @@ class PagedCache:
         d = dims
         if not k_pages.is_cuda:
             raise ValueError("k_pages must be on the GPU")
-        if d.dtype not in (PD_BF16, PD_FP32) or d.cache_dtype not in _TYPES:
+        four = d.cache_dtype == PD_FP4_E2M1
+        if d.dtype not in (PD_BF16, PD_FP32) or not (four or d.cache_dtype in _TYPES):
             raise ValueError(f"no element type {d.dtype} or cache type {d.cache_dtype}")
         self.device = k_pages.get_device()
         self._key = self._sizes(dims)
         self.tensors = (k_pages, v_pages, k_exp, v_exp, k_bounds, page_table, kv_len, new_rows)
-        if (d.cache_dtype == PD_FP8_E4M3) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
-            raise ValueError("k_exp and v_exp belong to a cache of PD_FP8_E4M3, and only to it")
+        if (four or d.cache_dtype == PD_FP8_E4M3) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
+            raise ValueError("k_exp and v_exp belong to a cache of PD_FP8_E4M3 or PD_FP4_E2M1, and only to it")
         self.type = _TYPES[d.dtype]
-        # E4M3 pages may also come as the bytes that they are.
-        page = k_pages.dtype if d.cache_dtype == PD_FP8_E4M3 and k_pages.dtype is torch.uint8 else _TYPES[d.cache_dtype]
+        # E4M3 pages may also come as the bytes that they are, as those of E2M1 do.
+        bytes_ = four or (d.cache_dtype == PD_FP8_E4M3 and k_pages.dtype is torch.uint8)
+        page = torch.uint8 if bytes_ else _TYPES[d.cache_dtype]
         pool = (d.n_pages, d.n_heads_kv, d.page_rows)
-        wanted = ((pool + (d.head_dim,), page), (pool + (d.head_dim,), page), (pool, torch.uint8), (pool, torch.uint8),
+        rows = pool + (d.head_dim // 2 if four else d.head_dim,)
+        exps = (pool[:2] + (d.head_dim // 32, d.page_rows) if four else pool, torch.uint8)
+        wanted = ((rows, page), (rows, page), exps, exps,
                   (pool[:2] + (2, d.head_dim), self.type), ((d.batch, d.max_pages), torch.int32),
                   ((d.batch,), torch.int32), ((d.batch,), torch.int32))
         self.c = PdPagedCache()

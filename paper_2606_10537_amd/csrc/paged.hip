@@ -145,6 +145,80 @@ hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
+// What a lane needs to write its 16 bytes of rows into a page: row `base` of the pool is the page's
+// row 0 (of one KV head), c the lane of a row.
+template <int CT, int D>
+struct CacheRow {
+  static constexpr int E = CT == kFp32 ? 4 : 8, L = D / E, EB = CT == kFp32 ? 4 : 2;
+  char* dst;
+  uint8_t* ex;
+  int c;
+  __device__ __forceinline__ CacheRow(const PagedArgs& p, int kv, long long base, int lane) : ex(nullptr), c(lane) {
+    char* pages = (char*)(kv ? p.v_pages : p.k_pages);
+    uint8_t* exps = kv ? p.v_exp : p.k_exp;
+    if constexpr (CT == kFp4) {
+      dst = pages + base * (D / 2) + c * 4;
+      ex = exps + base * (D / 32) + (c / 4) * p.R;   // exponent bytes of 32 channels lie by rows
+    } else if constexpr (CT == kFp8) {
+      dst = pages + base * D + c * 8;
+      ex = exps + base;
+    } else {
+      dst = pages + base * (D * EB) + c * 16;
+    }
+  }
+  // Writes row `slot` of the page, where `live`; x: the lane's 16 bytes, y: their elements.  All
+  // lanes of a row are active.
+  __device__ __forceinline__ void put(const Row16<CT != kFp32>& x, const float* y, int slot, bool live) const {
+    if constexpr (CT == kFp8 || CT == kFp4) {
+      float m = 0.f;
+      bool finite = true;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float t = fabsf(y[e]);
+        finite = finite && t < INFINITY;
+        m = fmaxf(m, t < INFINITY ? t : 0.f);
+      }
+      if constexpr (CT == kFp8) {
+        m = lanes_max<L>(m);
+        const uint32_t bits = __float_as_uint(m);
+        const int e2 = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
+        const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float z[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[e] = y[4 * k + e] * inv;
+            z[e] = fabsf(y[4 * k + e]) < INFINITY ? z[e] : NAN;
+          }
+          int v = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+          w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], v, true);
+        }
+        if (live) {
+          *(u32x2*)(dst + (long long)slot * D) = u32x2{w[0], w[1]};
+          if (c == 0) ex[slot] = (uint8_t)(e2 + 127);
+        }
+      } else {
+        // The group's four lanes: its maximum, or infinity where an element is not finite.
+        m = finite ? m : INFINITY;
+        m = fmaxf(m, dpp<0xb1>(m, m));
+        m = fmaxf(m, dpp<0x4e>(m, m));
+        const uint32_t bits = __float_as_uint(m);
+        const int e2 = min(max((int)(bits >> 23) - 129 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0), -100), 126);
+        const uint32_t w = to_fp4(y, exp_to_scale((uint32_t)(e2 + 127)));
+        if (live) {
+          *(uint32_t*)(dst + (long long)slot * (D / 2)) = w;
+          if ((c & 3) == 0) ex[slot] = m < INFINITY ? (uint8_t)(e2 + 127) : (uint8_t)255;
+        }
+      }
+    } else {
+      if (live) x.store_once(dst + (long long)slot * (D * EB));
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
 // Writing rows into the pages.
 //
 // One workgroup per (sequence, page that new rows fall into, KV head): the bounds of a
@@ -156,13 +230,15 @@ hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s) {
 //
 // Quantisation: e from the bits of the largest magnitude (448 = 1.75 * 2^8, so e is the
 // binary exponent minus 8, or one more where the mantissa exceeds 1.75), the
-// product with 2^-e is exact, and the conversion rounds to nearest even.
+// product with 2^-e is exact, and the conversion rounds to nearest even.  In 4 bits the largest
+// magnitude is that of 32 channels, four lanes in bf16 (6 = 1.5 * 2^2).
 //
 // NW: waves.  Eight where a page may take more than 64 new rows (pages of 256 rows, one head,
 // 4000 rows: 12.5 us, 16.2 with four, 11.9 with sixteen, which take 80 instead of 51 us for
 // prompts of four sequences of 32 heads over pages of 128 rows).
-template <bool BF16, bool FP8, int D, int NW>
+template <int CT, int D, int NW>
 __global__ __launch_bounds__(NW * 64) void paged_append_kernel(AppendArgs a) {
+  constexpr bool BF16 = CT != kFp32;
   constexpr int E = BF16 ? 8 : 4, L = D / E, HP = 64 / L, EB = BF16 ? 2 : 4;
   __shared__ float bound[NW / 2][2][D];
   const PagedArgs& p = a.c;
@@ -183,8 +259,7 @@ __global__ __launch_bounds__(NW * 64) void paged_append_kernel(AppendArgs a) {
   const char* src = (const char*)(kv ? a.v_new : a.k_new) + ((long long)h * D + c * E) * EB;
   const long long stride = (kv ? a.vs : a.ks) * EB;
   const long long base = ((long long)page * p.Hkv + h) * p.R;   // row of the pool
-  char* dst = (char*)(kv ? p.v_pages : p.k_pages) + (base * D + c * E) * (FP8 ? 1 : EB);
-  uint8_t* ex = FP8 ? (kv ? p.v_exp : p.k_exp) + base : nullptr;
+  const CacheRow<CT, D> to(p, kv, base, c);
   const bool bounds = p.k_bounds && kv == 0;
   const bool widen = (lo & (p.R - 1)) != 0;            // the page's row 0 is an older one
   // This thread's element of the bounds: the least keys, then the largest.
@@ -223,36 +298,7 @@ __global__ __launch_bounds__(NW * 64) void paged_append_kernel(AppendArgs a) {
           most[e] = fmaxf(most[e], y[e]);
         }
       }
-      if constexpr (FP8) {
-        float m = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float t = fabsf(y[e]);
-          m = fmaxf(m, t < INFINITY ? t : 0.f);
-        }
-        m = lanes_max<L>(m);
-        const uint32_t bits = __float_as_uint(m);
-        const int e2 = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
-        const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
-        uint32_t w[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float z[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            z[e] = y[4 * k + e] * inv;
-            z[e] = fabsf(y[4 * k + e]) < INFINITY ? z[e] : NAN;
-          }
-          int v = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-          w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], v, true);
-        }
-        if (live) {
-          *(u32x2*)(dst + (long long)slot * D) = u32x2{w[0], w[1]};
-          if (c == 0) ex[slot] = (uint8_t)(e2 + 127);
-        }
-      } else {
-        if (live) x[u].store_once(dst + (long long)slot * D * EB);
-      }
+      to.put(x[u], y, slot, live);
     }
   }
   if (!p.k_bounds) return;
@@ -284,19 +330,17 @@ __global__ __launch_bounds__(NW * 64) void paged_append_kernel(AppendArgs a) {
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
   const dim3 grid = grid_xy((long long)a.c.B * a.pages * a.c.Hkv);
   const bool tall = a.c.R > 64 && a.c.Ln > 64;
-#define PD_APPEND(BF, F8, DD)                                                                              \
+#define PD_APPEND(CT, DD)                                                                                  \
   do {                                                                                                     \
-    if (tall) hipLaunchKernelGGL((paged_append_kernel<BF, F8, DD, 8>), grid, dim3(512), 0, s, a);        \
-    else hipLaunchKernelGGL((paged_append_kernel<BF, F8, DD, 4>), grid, dim3(256), 0, s, a);               \
+    if (tall) hipLaunchKernelGGL((paged_append_kernel<CT, DD, 8>), grid, dim3(512), 0, s, a);            \
+    else hipLaunchKernelGGL((paged_append_kernel<CT, DD, 4>), grid, dim3(256), 0, s, a);                   \
   } while (0)
-  if (a.c.D == 128) {
-    if (a.c.fp8) PD_APPEND(true, true, 128);
-    else if (a.c.bf16) PD_APPEND(true, false, 128);
-    else PD_APPEND(false, false, 128);
-  } else {
-    if (a.c.fp8) PD_APPEND(true, true, 64);
-    else if (a.c.bf16) PD_APPEND(true, false, 64);
-    else PD_APPEND(false, false, 64);
+  const bool wide = a.c.D == 128;
+  switch (cache_type(a.c)) {
+    case kBf16: if (wide) PD_APPEND(kBf16, 128); else PD_APPEND(kBf16, 64); break;
+    case kFp8: if (wide) PD_APPEND(kFp8, 128); else PD_APPEND(kFp8, 64); break;
+    case kFp4: if (wide) PD_APPEND(kFp4, 128); else PD_APPEND(kFp4, 64); break;
+    default: if (wide) PD_APPEND(kFp32, 128); else PD_APPEND(kFp32, 64); break;
   }
 #undef PD_APPEND
   return hipGetLastError();
@@ -306,8 +350,9 @@ hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s) {
 // Reading rows back: a lane writes 16 bytes of the output, a wave consecutive
 // rows of one (sequence, head), which lie beside each other in the pages too.
 // Memory bounds it.
-template <bool BF16, bool FP8, int D>
+template <int CT, int D>
 __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a) {
+  constexpr bool BF16 = CT != kFp32;
   constexpr int E = BF16 ? 8 : 4, L = D / E, RP = 256 / L, EB = BF16 ? 2 : 4, U = 4;
   const PagedArgs& p = a.c;
   const int id = uniform((int)block_id());
@@ -333,7 +378,24 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a) {
   for (int kv = 0; kv < 2; ++kv) {
     const char* src = (const char*)(kv ? p.v_pages : p.k_pages);
     char* out = (char*)(kv ? a.v_out : a.k_out) + ((long long)bh * a.n * D + c * E) * EB;
-    if constexpr (FP8) {
+    if constexpr (CT == kFp4) {
+      const uint8_t* ex = kv ? p.v_exp : p.k_exp;
+      uint32_t w[U];
+      float s[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        w[u] = __builtin_nontemporal_load((const uint32_t*)(src + at[u] * (D / 2) + c * 4));
+        const int slot = (a.first + min(row0 + u * RP, end - 1)) & (p.R - 1);
+        s[u] = exp_to_scale(ex[(at[u] - slot) * (D / 32) + (long long)(c / 4) * p.R + slot]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        Row16<true> x;
+        x.v = from_fp4(w[u], s[u]);
+        if (bad[u]) x.nan();
+        if (row0 + u * RP < end) x.store_once(out + (long long)(row0 + u * RP) * D * EB);
+      }
+    } else if constexpr (CT == kFp8) {
       const uint8_t* ex = kv ? p.v_exp : p.k_exp;
       u32x2 w[U];
       float s[U];
@@ -372,20 +434,23 @@ __global__ __launch_bounds__(256) void paged_read_kernel(ReadArgs a) {
   }
 }
 
-template <bool BF16, bool FP8, int D>
+template <int CT, int D>
 hipError_t read_of(ReadArgs a, hipStream_t s) {
-  constexpr int rows = 256 / (D / (BF16 ? 8 : 4)) * 4;
+  constexpr int rows = 256 / (D / (CT == kFp32 ? 4 : 8)) * 4;
   const int blocks = (a.n + rows - 1) / rows;
   a.by_blocks = fast_div(blocks);
-  hipLaunchKernelGGL((paged_read_kernel<BF16, FP8, D>), grid_xy((long long)a.c.B * a.c.Hkv * blocks), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((paged_read_kernel<CT, D>), grid_xy((long long)a.c.B * a.c.Hkv * blocks), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s) {
   const bool wide = a.c.D == 128;
-  if (a.c.fp8) return wide ? read_of<true, true, 128>(a, s) : read_of<true, true, 64>(a, s);
-  if (a.c.bf16) return wide ? read_of<true, false, 128>(a, s) : read_of<true, false, 64>(a, s);
-  return wide ? read_of<false, false, 128>(a, s) : read_of<false, false, 64>(a, s);
+  switch (cache_type(a.c)) {
+    case kBf16: return wide ? read_of<kBf16, 128>(a, s) : read_of<kBf16, 64>(a, s);
+    case kFp8: return wide ? read_of<kFp8, 128>(a, s) : read_of<kFp8, 64>(a, s);
+    case kFp4: return wide ? read_of<kFp4, 128>(a, s) : read_of<kFp4, 64>(a, s);
+    default: return wide ? read_of<kFp32, 128>(a, s) : read_of<kFp32, 64>(a, s);
+  }
 }
 
 // ---------------------------------------------------------------------------

@@ -33,9 +33,10 @@ pd_status check_paged_dims(const pd_paged_dims* d) {
     return fail(PD_ERR_UNSUPPORTED, "head_dim=%d must be 64 or 128", d->head_dim);
   if (d->dtype != PD_BF16 && d->dtype != PD_FP32)
     return fail(PD_ERR_UNSUPPORTED, "dtype=%d is neither PD_BF16 nor PD_FP32", d->dtype);
-  if (d->cache_dtype != d->dtype && !(d->cache_dtype == PD_FP8_E4M3 && d->dtype == PD_BF16))
-    return fail(PD_ERR_UNSUPPORTED, "cache_dtype=%d must be dtype=%d, or PD_FP8_E4M3 with PD_BF16", d->cache_dtype,
-                d->dtype);
+  if (d->cache_dtype != d->dtype &&
+      !((d->cache_dtype == PD_FP8_E4M3 || d->cache_dtype == PD_FP4_E2M1) && d->dtype == PD_BF16))
+    return fail(PD_ERR_UNSUPPORTED, "cache_dtype=%d must be dtype=%d, or PD_FP8_E4M3 or PD_FP4_E2M1 with PD_BF16",
+                d->cache_dtype, d->dtype);
   if (d->page_rows < 16 || d->page_rows > 256 || (d->page_rows & (d->page_rows - 1)) != 0)
     return fail(PD_ERR_BAD_DIMS, "page_rows=%d must be 16, 32, 64, 128 or 256", d->page_rows);
   if (d->n_pages < 1) return fail(PD_ERR_BAD_DIMS, "n_pages=%d must be >= 1", d->n_pages);
@@ -50,11 +51,11 @@ pd_status check_paged_dims(const pd_paged_dims* d) {
 
 pd_status check_cache(const pd_paged_dims* d, const pd_paged_cache* c, bool pages, bool bounds) {
   if (!c) return fail(PD_ERR_NULL_PTR, "cache is NULL");
-  const bool fp8 = d->cache_dtype == PD_FP8_E4M3;
+  const bool scaled = d->cache_dtype == PD_FP8_E4M3 || d->cache_dtype == PD_FP4_E2M1;
   if (pages) {
     PD_REQUIRE_PTR(c->k_pages);
     PD_REQUIRE_PTR(c->v_pages);
-    if (fp8) {
+    if (scaled) {
       PD_REQUIRE_PTR(c->k_exp);
       PD_REQUIRE_PTR(c->v_exp);
     }
@@ -99,6 +100,7 @@ pd::PagedArgs paged_args(const pd_paged_dims* d, const pd_paged_cache* c) {
   a.causal = d->causal;
   a.bf16 = d->dtype == PD_BF16;
   a.fp8 = d->cache_dtype == PD_FP8_E4M3;
+  a.fp4 = d->cache_dtype == PD_FP4_E2M1;
   const float scale = d->sm_scale > 0.f ? d->sm_scale : 1.0f / std::sqrt((float)d->head_dim);
   a.scale_log2 = scale * 1.4426950408889634f;
   return a;

@@ -301,20 +301,20 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   }
 }
 
-enum { kBf16 = 0, kFp8 = 1, kFp32 = 2 };
-
 template <int D, int CT>
 struct PagedShape {
   static constexpr int KS = CT == kFp32 ? 16 : 32;          // keys of a step
   static constexpr int H = KS / 16;                         // groups of 16 keys
-  static constexpr int CB = CT == kFp32 ? 4 : CT == kFp8 ? 1 : 2;
-  static constexpr int NK = D * CB / 64;                    // 16-byte reads of a lane for 16 keys
+  static constexpr int RB = CT == kFp32 ? 4 * D : CT == kFp8 ? D : CT == kFp4 ? D / 2 : 2 * D;   // bytes of a row
+  static constexpr int NK = (RB + 63) / 64;                 // 16-byte reads of a lane for 16 keys (4 bits, d = 64: 8 bytes)
   static constexpr int VR = CT == kFp32 ? 4 : 8;            // V rows of a lane
-  static constexpr int VW = D * CB / 64;                    // dwords of each
+  static constexpr int VW = (RB + 63) / 64;                 // dwords of each
   static constexpr int E = CT == kFp32 ? 4 : D / 16;        // neighbouring channels of a lane
   static constexpr int NT = D / 16;                         // products of P V
-  // First channel of result row m (bf16 and E4M3).
-  static __device__ __forceinline__ int base(int m) { return CT == kFp8 ? 2 * E * (m & 7) + E * (m >> 3) : E * m; }
+  // First channel of result row m (all but fp32).
+  static __device__ __forceinline__ int base(int m) {
+    return CT == kFp8 || (CT == kFp4 && D == 64) ? 2 * E * (m & 7) + E * (m >> 3) : E * m;
+  }
   static constexpr int BK = kPagedWaves * KS;
 };
 
@@ -325,6 +325,7 @@ struct PagedStep {
   u32x4 k[S::H][S::NK];
   uint32_t v[S::VR][S::VW];      // E4M3: read 2 j + i of 16 keys, rows 2 j and 2 j + 1 in a line
   uint32_t ex;                   // exponent bytes of four keys (see load)
+  uint32_t kx[S::H], vx[S::H];   // 4 bits: exponent byte of the lane's K group, those of its V group of four keys
   int pos[S::H];                 // position of the first key of each 16
 };
 
@@ -370,7 +371,7 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 template <int D, int CT, int RT, bool STREAM>
 __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
-  constexpr int H = S::H, CB = S::CB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
+  constexpr int H = S::H, RB = S::RB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
   __shared__ float lds_o[kPagedWaves][16][OP];
   __shared__ float lds_ml[kPagedWaves][RT * 16][2];
@@ -406,8 +407,9 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     } else {
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        // bf16 keys: read i of a lane is channels 32 i + 8 g..; E4M3 keys: 64 (i/2) + 16 g + 8 (i%2)..
-        const int ch = CT == kBf16 ? 32 * i + 8 * g4 : 64 * (i / 2) + 16 * g4 + 8 * (i & 1);
+        // bf16 keys: read i of a lane is channels 32 i + 8 g..; E4M3 keys: 64 (i/2) + 16 g + 8 (i%2)..;
+        // E2M1 keys: d/4 g + 8 i..
+        const int ch = CT == kBf16 ? 32 * i + 8 * g4 : CT == kFp8 ? 64 * (i / 2) + 16 * g4 + 8 * (i & 1) : D / 4 * g4 + 8 * i;
         qb[t][i] = *(const bf16x8*)((const uint16_t*)a.q + q_el + ch);
       }
     }
@@ -461,11 +463,23 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       const int page = __builtin_amdgcn_readlane(at_page[h], i & 63);
       s.pos[h] = __builtin_amdgcn_readlane(at_pos[h], i & 63);
       const long long row = ((long long)page * p.Hkv + g) * page_rows + (s.pos[h] & (p.R - 1));
-      const char* kp = (const char*)p.k_pages + row * (D * CB) + n * (D * CB) + 16 * g4;
+      const char* kp = (const char*)p.k_pages + row * RB + n * RB + (RB < 64 ? RB / 4 : 16) * g4;
+      if constexpr (RB < 64) {
+        const u32x2 w = fetch<STREAM>((const u32x2*)kp);
+        s.k[h][0] = u32x4{w[0], w[1], 0, 0};
+      } else {
 #pragma unroll
-      for (int j = 0; j < NK; ++j) s.k[h][j] = fetch<STREAM>((const u32x4*)(kp + 64 * j));
-      const char* vp = (const char*)p.v_pages + row * (D * CB) + g4 * (4 * D * CB);
-      if constexpr (CT == kFp8) {
+        for (int j = 0; j < NK; ++j) s.k[h][j] = fetch<STREAM>((const u32x4*)(kp + 64 * j));
+      }
+      const char* vp = (const char*)p.v_pages + row * RB + g4 * (4 * RB);
+      if constexpr (CT == kFp4) {
+        // Eight neighbouring channels of four keys; in d = 64 lanes n and n ^ 8 read the same and keep four each.
+        const long long row_exp = (row - (s.pos[h] & (p.R - 1))) * (D / 32) + (s.pos[h] & (p.R - 1));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s.v[4 * h + j][0] = fetch<STREAM>((const uint32_t*)(vp + j * RB) + (D == 64 ? n & 7 : n));
+        s.kx[h] = p.k_exp[row_exp + (long long)(D == 64 ? g4 >> 1 : g4) * p.R + n];
+        s.vx[h] = *(const uint32_t*)(p.v_exp + row_exp + (long long)(D == 64 ? (n & 7) >> 2 : n >> 2) * p.R + 4 * g4);
+      } else if constexpr (CT == kFp8) {
         // Lanes n and n ^ 8 read twice the channels that they need, of two keys each, and swap
         // halves later: loads of 8 bytes a lane were twice as many (one sequence of 128K keys
         // with 8 heads 50.8 us, now 49.0; 64 ragged ones 380, now 377).
@@ -483,11 +497,11 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           uint32_t* w = s.v[4 * h + j];
           if constexpr (CT == kFp32) {
 #pragma unroll
-            for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 256 * u + 16 * n));
+            for (int u = 0; u < VW / 4; ++u) *(u32x4*)(w + 4 * u) = fetch<STREAM>((const u32x4*)(vp + j * RB + 256 * u + 16 * n));
           } else if constexpr (VW == 4) {
-            *(u32x4*)w = fetch<STREAM>((const u32x4*)(vp + j * (D * CB) + 16 * n));
+            *(u32x4*)w = fetch<STREAM>((const u32x4*)(vp + j * RB + 16 * n));
           } else {
-            *(u32x2*)w = fetch<STREAM>((const u32x2*)(vp + j * (D * CB) + 8 * n));
+            *(u32x2*)w = fetch<STREAM>((const u32x2*)(vp + j * RB + 8 * n));
           }
         }
       }
@@ -506,7 +520,14 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     // an infinity or a NaN.
     constexpr int W = CT == kFp32 ? VW : D / 32;
     uint32_t v[VR][W], ke[H], ve[H];
-    if constexpr (CT == kFp8) {
+    if constexpr (CT == kFp4) {
+#pragma unroll
+      for (int j = 0; j < VR; ++j) {
+        const u32x4 x = from_fp4(D == 64 ? s.v[j][0] >> (2 * (n & 8)) : s.v[j][0], exp_to_scale((s.vx[j / 4] >> (8 * (j % 4))) & 255));
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[j][w] = x[w];
+      }
+    } else if constexpr (CT == kFp8) {
 #pragma unroll
       for (int h = 0; h < H; ++h) {
         ke[h] = row_lane<0>(s.ex, h);
@@ -593,6 +614,10 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
         } else if constexpr (CT == kBf16) {
 #pragma unroll
           for (int i = 0; i < NK; ++i) sc[h] = mfma16x16x32(__builtin_bit_cast(bf16x8, s.k[h][i]), qb[t][i], sc[h]);
+        } else if constexpr (CT == kFp4) {
+#pragma unroll
+          for (int i = 0; i < D / 32; ++i)
+            sc[h] = mfma16x16x32(__builtin_bit_cast(bf16x8, from_fp4(s.k[h][0][i], exp_to_scale(s.kx[h]))), qb[t][i], sc[h]);
         } else {
 #pragma unroll
           for (int i = 0; i < NK; ++i)
@@ -919,9 +944,12 @@ hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
   const bool wide = a.c.D == 128;
-  if (a.c.fp8) return wide ? paged_attn_of<128, kFp8>(a, s) : paged_attn_of<64, kFp8>(a, s);
-  if (a.c.bf16) return wide ? paged_attn_of<128, kBf16>(a, s) : paged_attn_of<64, kBf16>(a, s);
-  return wide ? paged_attn_of<128, kFp32>(a, s) : paged_attn_of<64, kFp32>(a, s);
+  switch (cache_type(a.c)) {
+    case kBf16: return wide ? paged_attn_of<128, kBf16>(a, s) : paged_attn_of<64, kBf16>(a, s);
+    case kFp8: return wide ? paged_attn_of<128, kFp8>(a, s) : paged_attn_of<64, kFp8>(a, s);
+    case kFp4: return wide ? paged_attn_of<128, kFp4>(a, s) : paged_attn_of<64, kFp4>(a, s);
+    default: return wide ? paged_attn_of<128, kFp32>(a, s) : paged_attn_of<64, kFp32>(a, s);
+  }
 }
 
 }  // namespace pd

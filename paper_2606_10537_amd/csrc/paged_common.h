@@ -39,8 +39,25 @@ struct Row16 {
   }
 };
 
-// 2^e of an exponent byte e + 127 (27..247).
+// 2^e of an exponent byte e + 127 (27..247, in 4 bits ..253; 255, a group that is NaN, is what the conversions from 4 bits
+// take for NaN).
 __device__ __forceinline__ float exp_to_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight E2M1 values times a power of two, to and from bf16 or fp32: element i is in bits 4 i.  Rounded to
+// nearest even, at most +-6; from 4 bits the results are exact.
+__device__ __forceinline__ u32x4 from_fp4(uint32_t w, float scale) {
+  return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+__device__ __forceinline__ uint32_t to_fp4(const float* y, float scale) {
+  uint32_t w = 0;
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+}
 
 // Rows and new rows of a sequence, within what the cache and the call have room for.
 __device__ __forceinline__ int paged_len(const PagedArgs& p, int b) {

@@ -43,9 +43,13 @@ struct PagedArgs {
   void* k_bounds;
   const int32_t *page_table, *kv_len, *new_rows;
   int B, Ln, Hq, Hkv, G, D, R, log2R, n_pages, max_pages, causal;
-  bool bf16, fp8;        // new rows and outputs in bf16 (else fp32); pages in E4M3
+  bool bf16, fp8, fp4;   // new rows and outputs in bf16 (else fp32); pages in E4M3, in E2M1
   float scale_log2;      // softmax scale * log2(e)
 };
+
+// How the pages hold the elements.
+enum { kBf16 = 0, kFp8 = 1, kFp32 = 2, kFp4 = 3 };
+inline int cache_type(const PagedArgs& p) { return p.fp8 ? kFp8 : p.fp4 ? kFp4 : p.bf16 ? kBf16 : kFp32; }
 
 struct AppendArgs {
   PagedArgs c;
