@@ -471,6 +471,28 @@ pd_status pd_paged_attn(const pd_paged_dims *dims, const pd_paged_cache *cache, 
                         const int32_t *page_idx, int32_t top_k, void *o, float *lse, void *workspace,
                         size_t ws_bytes, void *stream);
 
+/*
+ * pd_paged_attn within a sliding window, with the first positions visible
+ * throughout: row r < new_rows[b], which is position p = kv_len[b] - new_rows[b] + r,
+ * attends to the positions j that pd_paged_attn lets it see (j <= p, or all with
+ * causal = 0) and that lie in its window, j > p - window, or among the first,
+ * j < n_sinks.  With causal = 0 a window bounds what lies before a row; the positions
+ * behind it, which are new rows, are all seen.  Pages none of whose positions a row
+ * of the call sees are not read, and neither are their entries in page_table, so that they may be
+ * given to other sequences.  Everything else is as for pd_paged_attn over all
+ * pages: o, lse, rows that see nothing, page ids outside the pool, values that are
+ * not finite, rounding.
+ * Sizes: window >= 1, n_sinks >= 0 (those beyond all positions count as all).
+ * workspace: >= pd_paged_window_workspace_bytes(dims, window, n_sinks) bytes (may be
+ * 0, then workspace may be NULL), which grow with the window and not with max_pages.
+ */
+pd_status pd_paged_window_attn(const pd_paged_dims *dims, const pd_paged_cache *cache, const void *q,
+                               int32_t window, int32_t n_sinks, void *o, float *lse, void *workspace,
+                               size_t ws_bytes, void *stream);
+
+/* Workspace bytes of pd_paged_window_attn.  Returns 0 for invalid arguments. */
+size_t pd_paged_window_workspace_bytes(const pd_paged_dims *dims, int32_t window, int32_t n_sinks);
+
 /* Workspace bytes for `which` = 0 pd_paged_select, 1 pd_paged_attn (top_k = 0:
  * over all pages).  Returns 0 for invalid arguments. */
 size_t pd_paged_workspace_bytes(const pd_paged_dims *dims, int32_t top_k, int32_t which);

@@ -107,8 +107,9 @@ def select_ref(score, top_k, n_first, n_last):
     return sorted(j for _, _, j in sorted(key)[:top_k])
 
 
-def attn_ref(q, k, v, ends, scale, pos=None):
-    """q [rows, d], k, v [keys, d]; row r sees the keys whose position (pos, or their index) is below ends[r].
+def attn_ref(q, k, v, ends, scale, pos=None, lows=None, first=0):
+    """q [rows, d], k, v [keys, d]; row r sees the keys whose position (pos, or their index) is below ends[r], and with
+    lows at least lows[r] or below first.
 
     Returns o, lse, mass (sum of the weights times |v|, per element) and spread (the largest scale * sum |q_i k_i| of
     a visible key), which the tolerances of the tests are made of."""
@@ -118,6 +119,8 @@ def attn_ref(q, k, v, ends, scale, pos=None):
     lse, spread = np.full(len(q), -np.inf), np.zeros(len(q))
     for r in range(len(q)):
         seen = pos < ends[r]
+        if lows is not None:
+            seen = seen & ((pos >= lows[r]) | (pos < first))
         if not seen.any():
             continue
         s = scale * (k[seen] @ q[r])

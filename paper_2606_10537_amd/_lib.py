@@ -22,7 +22,8 @@ EXPORTS = ["pd_prefill_chunks", "pd_score_select", "pd_sparse_decode_attn", "pd_
            "pd_version", "pd_mfma_rate_probe", "pd_score_select_static", "pd_gather_selected",
            "pd_sparse_decode_attn_compact", "pd_compact_workspace_bytes", "pd_select_ranked",
            "pd_gather_joint", "pd_score_select_noalloc", "pd_qk_norm_rope", "pd_paged_append", "pd_paged_read",
-           "pd_paged_select", "pd_paged_attn", "pd_paged_workspace_bytes"]
+           "pd_paged_select", "pd_paged_attn", "pd_paged_workspace_bytes", "pd_paged_window_attn",
+           "pd_paged_window_workspace_bytes"]
 
 
 class PdError(RuntimeError):
@@ -146,6 +147,10 @@ def load(path: str = LIB_PATH):
     lib.pd_paged_select.restype = ctypes.c_int
     lib.pd_paged_attn.argtypes = [pp, cp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.pd_paged_attn.restype = ctypes.c_int
+    lib.pd_paged_window_attn.argtypes = [pp, cp, vp, i32, i32, vp, vp, vp, sz, vp]
+    lib.pd_paged_window_attn.restype = ctypes.c_int
+    lib.pd_paged_window_workspace_bytes.argtypes = [pp, i32, i32]
+    lib.pd_paged_window_workspace_bytes.restype = sz
     lib.pd_paged_workspace_bytes.argtypes = [pp, i32, i32]
     lib.pd_paged_workspace_bytes.restype = sz
     lib.pd_version.argtypes = []
@@ -481,3 +486,27 @@ def pd_paged_attn(dims: PagedDims, cache: PagedCache, q, o, lse=None, page_idx=N
     _check(load().pd_paged_attn(ctypes.byref(dims), c, _checked("q", q, shape, cache.type, dev), ip, top_k,
                                 _checked("o", o, shape, cache.type, dev), lp, *_space(workspace, dev),
                                 _launch_stream(stream, dev)))
+
+
+def pd_paged_window_workspace_bytes(dims: PagedDims, window, n_sinks=0) -> int:
+    _window_sizes(window, n_sinks)
+    return load().pd_paged_window_workspace_bytes(ctypes.byref(dims), window, n_sinks)
+
+
+def _window_sizes(window, n_sinks):
+    if not -_FAR <= window < _FAR or not -_FAR <= n_sinks < _FAR:
+        raise ValueError(f"window={window} and n_sinks={n_sinks} must fit 32 bits")
+
+
+def pd_paged_window_attn(dims: PagedDims, cache: PagedCache, q, window, n_sinks, o, lse=None, workspace=None,
+                         stream=None):
+    """Attention of the new rows q [B, L_n, H_q, d] over the last `window` positions up to their own and the first
+    n_sinks (see include/pd.h); lse [B, H_q, L_n] fp32 or None."""
+    c, dev = cache._for(dims), cache.device
+    _window_sizes(window, n_sinks)
+    B, L, hq = dims.batch, dims.new_len, dims.n_heads_q
+    shape = (B, L, hq, dims.head_dim)
+    lp = None if lse is None else _checked("lse", lse, (B, hq, L), _TYPES[PD_FP32], dev)
+    _check(load().pd_paged_window_attn(ctypes.byref(dims), c, _checked("q", q, shape, cache.type, dev), window, n_sinks,
+                                       _checked("o", o, shape, cache.type, dev), lp, *_space(workspace, dev),
+                                       _launch_stream(stream, dev)))

@@ -118,12 +118,12 @@ struct AttnPlan {
   size_t o_bytes, ml_bytes, unit_bytes, total;
   bool planned;
 };
-pd_status attn_plan(const pd_paged_dims* d, int top_k, AttnPlan* p) {
+pd_status attn_plan(const pd_paged_dims* d, int top_k, long long most_keys, AttnPlan* p) {
   const long long rows = (long long)(d->n_heads_q / d->n_heads_kv) * d->new_len;
   p->row_blocks = cdiv(rows, pd::kPagedRows);
   p->part_rows = (int)std::min<long long>(rows, pd::kPagedRows);
   const long long units = (long long)d->batch * d->n_heads_kv * p->row_blocks;
-  const long long keys = (long long)(top_k > 0 ? top_k : d->max_pages) * d->page_rows;
+  const long long keys = std::min((long long)(top_k > 0 ? top_k : d->max_pages) * d->page_rows, most_keys);
   const long long blocks = cdiv(keys, pd::paged_block_keys(d->dtype == PD_FP32));
   if (units >= kMaxGrid / 2 || (double)units * (double)blocks >= 9e18)
     return fail(PD_ERR_BAD_DIMS, "attention of batch=%d with new_len=%d is too large for one launch", d->batch,
@@ -171,6 +171,64 @@ pd_status check_attn_pages(const pd_paged_dims* d, const int32_t* page_idx, int 
                 d->max_pages);
   if (page_idx && !aligned16(page_idx)) return fail(PD_ERR_MISALIGNED, "pointer 'page_idx' is not 16-byte aligned");
   return PD_OK;
+}
+
+struct Window {
+  int window, n_sinks, keys;   // keys: of a row block, see PagedAttnArgs
+  long long most_keys;         // of any
+};
+pd_status check_window(int window, int n_sinks) {
+  if (window < 1) return fail(PD_ERR_BAD_DIMS, "window=%d must be >= 1", window);
+  if (n_sinks < 0) return fail(PD_ERR_BAD_DIMS, "n_sinks=%d must be >= 0", n_sinks);
+  return PD_OK;
+}
+Window window_of(const pd_paged_dims* d, int window, int n_sinks) {
+  // Beyond all positions and new rows a window or a count has no further effect.
+  constexpr long long most = kMaxPositions + (1 << 24);
+  Window w{};
+  w.window = (int)std::min<long long>(window, most);
+  w.n_sinks = (int)std::min<long long>(n_sinks, kMaxPositions);
+  const int G = d->n_heads_q / d->n_heads_kv;
+  const long long rows = std::min<long long>(d->new_len, (pd::kPagedRows + G - 1) / G + 1);   // new rows of a row block
+  const long long keys = pd::paged_window_keys(w.window, w.n_sinks, d->causal ? rows : 0);
+  w.keys = (int)std::min<long long>(keys, kMaxPositions);
+  w.most_keys = w.keys + (d->causal ? 0 : (long long)d->new_len);
+  return w;
+}
+
+pd_status launch_attn(const pd_paged_dims* d, const pd_paged_cache* cache, const void* q, const int32_t* page_idx,
+                      int top_k, const Window* w, void* o, float* lse, void* workspace, size_t ws_bytes,
+                      void* stream) {
+  AttnPlan plan;
+  PD_RETURN_IF(attn_plan(d, top_k, w ? w->most_keys : kMaxPositions, &plan));
+  PD_RETURN_IF(check_ws(workspace, ws_bytes, plan.total));
+  pd::PagedAttnArgs a{};
+  a.c = paged_args(d, cache);
+  a.q = q;
+  a.page_idx = page_idx;
+  a.top_k = top_k;
+  if (w) {
+    a.window = w->window;
+    a.n_sinks = w->n_sinks;
+    a.window_keys = w->keys;
+  }
+  a.o = o;
+  a.lse = lse;
+  a.o_part = (float*)workspace;
+  a.ml_part = (float*)((char*)workspace + plan.o_bytes);
+  a.unit = (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes);
+  a.plan = plan.planned ? (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes + plan.unit_bytes) : nullptr;
+  a.row_blocks = plan.row_blocks;
+  a.part_rows = plan.part_rows;
+  a.max_chunks = plan.max_chunks;
+  a.per_part = 1.0f / plan.parts;
+  a.grid = plan.grid;
+  a.by_group = pd::fast_div(a.c.G);
+  a.by_heads = pd::fast_div(a.c.Hkv);
+  a.by_rows = pd::fast_div(a.c.G * a.c.Ln);
+  a.by_blocks = pd::fast_div(a.row_blocks);
+  a.by_units = pd::fast_div(a.c.Hkv * a.row_blocks);
+  return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");
 }
 
 }  // namespace
@@ -315,39 +373,32 @@ pd_status pd_paged_attn(const pd_paged_dims* d, const pd_paged_cache* cache, con
   PD_REQUIRE_PTR(q);
   PD_REQUIRE_PTR(o);
   if (lse && !aligned16(lse)) return fail(PD_ERR_MISALIGNED, "pointer 'lse' is not 16-byte aligned");
-  AttnPlan plan;
-  PD_RETURN_IF(attn_plan(d, top_k, &plan));
-  PD_RETURN_IF(check_ws(workspace, ws_bytes, plan.total));
-  pd::PagedAttnArgs a{};
-  a.c = paged_args(d, cache);
-  a.q = q;
-  a.page_idx = page_idx;
-  a.top_k = top_k;
-  a.o = o;
-  a.lse = lse;
-  a.o_part = (float*)workspace;
-  a.ml_part = (float*)((char*)workspace + plan.o_bytes);
-  a.unit = (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes);
-  a.plan = plan.planned ? (int32_t*)((char*)workspace + plan.o_bytes + plan.ml_bytes + plan.unit_bytes) : nullptr;
-  a.row_blocks = plan.row_blocks;
-  a.part_rows = plan.part_rows;
-  a.max_chunks = plan.max_chunks;
-  a.per_part = 1.0f / plan.parts;
-  a.grid = plan.grid;
-  a.by_group = pd::fast_div(a.c.G);
-  a.by_heads = pd::fast_div(a.c.Hkv);
-  a.by_rows = pd::fast_div(a.c.G * a.c.Ln);
-  a.by_blocks = pd::fast_div(a.row_blocks);
-  a.by_units = pd::fast_div(a.c.Hkv * a.row_blocks);
-  return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");
+  return launch_attn(d, cache, q, page_idx, top_k, nullptr, o, lse, workspace, ws_bytes, stream);
 }
 
+pd_status pd_paged_window_attn(const pd_paged_dims* d, const pd_paged_cache* cache, const void* q, int32_t window,
+                               int32_t n_sinks, void* o, float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  PD_RETURN_IF(check_paged_dims(d));
+  PD_RETURN_IF(check_window(window, n_sinks));
+  PD_RETURN_IF(check_cache(d, cache, true, false));
+  PD_REQUIRE_PTR(q);
+  PD_REQUIRE_PTR(o);
+  if (lse && !aligned16(lse)) return fail(PD_ERR_MISALIGNED, "pointer 'lse' is not 16-byte aligned");
+  const Window w = window_of(d, window, n_sinks);
+  return launch_attn(d, cache, q, nullptr, 0, &w, o, lse, workspace, ws_bytes, stream);
+}
 size_t pd_paged_workspace_bytes(const pd_paged_dims* d, int32_t top_k, int32_t which) {
   if (check_paged_dims(d) != PD_OK || top_k < 0 || top_k > d->max_pages) return 0;
   if (which == 0) return check_select_dims(d, top_k) == PD_OK ? select_bytes(d) : 0;
   if (which != 1) return 0;
   AttnPlan plan;
-  return attn_plan(d, top_k, &plan) == PD_OK ? plan.total : 0;
+  return attn_plan(d, top_k, kMaxPositions, &plan) == PD_OK ? plan.total : 0;
+}
+
+size_t pd_paged_window_workspace_bytes(const pd_paged_dims* d, int32_t window, int32_t n_sinks) {
+  if (check_paged_dims(d) != PD_OK || check_window(window, n_sinks) != PD_OK) return 0;
+  AttnPlan plan;
+  return attn_plan(d, 0, window_of(d, window, n_sinks).most_keys, &plan) == PD_OK ? plan.total : 0;
 }
 
 }  // extern "C"

@@ -67,14 +67,19 @@ struct PagedPart {
 struct PagedSeq {
   int len, n_new, blocks;
 };
-template <int BK>
+template <int BK, bool WIN>
 __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int b) {
   const PagedArgs& p = a.c;
   // Both loads in flight at once, also where there is no such sequence.
   const int at = b < p.B ? b : 0;
   const int len = p.kv_len[at], n_new = p.new_rows ? p.new_rows[at] : p.Ln;
   PagedSeq s{min(max(len, 0), p.max_pages << p.log2R), min(max(n_new, 0), p.Ln), 0};
-  if (b < p.B && s.len > 0 && s.n_new > 0) s.blocks = ((a.page_idx ? a.top_k << p.log2R : s.len) + BK - 1) / BK;
+  if (b < p.B && s.len > 0 && s.n_new > 0) {
+    int keys = a.page_idx ? a.top_k << p.log2R : s.len;
+    // A window: what a row block's keys are at most, in groups of 16.
+    if constexpr (WIN) keys = min((s.len + 15) & ~15, a.window_keys + (p.causal ? 0 : s.n_new));
+    s.blocks = (keys + BK - 1) / BK;
+  }
   return s;
 }
 
@@ -129,7 +134,7 @@ __device__ __forceinline__ int wave_most(int x) {
 // where walking all lengths would cost each wave more than this launch: quota, parts of the first
 // turn; then for every 64 sequences the parts of the first turn, and of both, up to their end.
 // One workgroup.
-template <int BK>
+template <int BK, bool WIN>
 __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
   __shared__ float sums[16];
   __shared__ int tops[16], whole[1024], parts[1024], ends[2][16];
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
   float all = 0.f;
   int most = 0;
   for (int i = wave; i < n; i += 16) {
-    const int x = paged_seq<BK>(a, 64 * i + lane).blocks;
+    const int x = paged_seq<BK, WIN>(a, 64 * i + lane).blocks;
     all += (float)wave_sum(x);
     most = max(most, wave_most(x));
   }
@@ -154,7 +159,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
   }
   const int quota = paged_quota(a, all * (float)units, most);
   for (int i = wave; i < n; i += 16) {
-    const PagedCut c = paged_cut(a, quota, 64 * i + lane, paged_seq<BK>(a, 64 * i + lane));
+    const PagedCut c = paged_cut(a, quota, 64 * i + lane, paged_seq<BK, WIN>(a, 64 * i + lane));
     const int w = wave_sum(c.whole), x = wave_sum(c.parts);
     if (lane == 0) {
       whole[i] = w;
@@ -186,7 +191,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedAttnArgs a) {
   }
 }
 
-template <int BK>
+template <int BK, bool WIN>
 __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find, int lane) {
   const PagedArgs& p = a.c;
   const int units = p.Hkv * a.row_blocks;
@@ -213,7 +218,7 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
   if (a.max_chunks == 1) {   // one part a unit
     r.b = a.by_units.quot(find);
     if (r.b >= p.B) return r;
-    const PagedSeq s = paged_seq<BK>(a, r.b);
+    const PagedSeq s = paged_seq<BK, WIN>(a, r.b);
     r.len = s.len;
     r.n_new = s.n_new;
     r.g = place(a.by_units.rem(find, r.b), 1);
@@ -247,20 +252,20 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
         break;
       }
     }
-    s = paged_seq<BK>(a, b0 + lane);
+    s = paged_seq<BK, WIN>(a, b0 + lane);
   } else {
-    const PagedSeq head = s = paged_seq<BK>(a, lane);
+    const PagedSeq head = s = paged_seq<BK, WIN>(a, lane);
     float all = 0.f;
     int most = 0;
     for (int c0 = 0; c0 < p.B; c0 += 64) {
-      const int n = c0 == 0 ? head.blocks : paged_seq<BK>(a, c0 + lane).blocks;
+      const int n = c0 == 0 ? head.blocks : paged_seq<BK, WIN>(a, c0 + lane).blocks;
       all += (float)wave_sum(n);
       most = max(most, wave_most(n));
     }
     quota = paged_quota(a, all * (float)units, most);
     first_turn = 0;
     for (int c0 = 0; c0 < p.B; c0 += 64)
-      first_turn += wave_sum(paged_cut(a, quota, c0 + lane, c0 == 0 ? head : paged_seq<BK>(a, c0 + lane)).whole);
+      first_turn += wave_sum(paged_cut(a, quota, c0 + lane, c0 == 0 ? head : paged_seq<BK, WIN>(a, c0 + lane)).whole);
     first_turn *= units;
     second = find >= first_turn;
     if (second) find -= first_turn;
@@ -297,7 +302,7 @@ __device__ __forceinline__ PagedPart paged_find(const PagedAttnArgs& a, int find
     before_all = __builtin_amdgcn_readlane(incl_all, 63);
     b0 += 64;
     if (b0 >= p.B) return r;
-    s = paged_seq<BK>(a, b0 + lane);
+    s = paged_seq<BK, WIN>(a, b0 + lane);
   }
 }
 
@@ -327,6 +332,7 @@ struct PagedStep {
   uint32_t ex;                   // exponent bytes of four keys (see load)
   uint32_t kx[S::H], vx[S::H];   // 4 bits: exponent byte of the lane's K group, those of its V group of four keys
   int pos[S::H];                 // position of the first key of each 16
+  bool bad[S::H];                // windows: their page lies outside the pool
 };
 
 // Over the four lanes n, 16 + n, 32 + n, 48 + n of a query row: halves, then neighbouring rows
@@ -368,7 +374,7 @@ constexpr int kFarPos = 1 << 30;   // the position of keys that are not there
 // against 723 us, 64 ragged sequences in 8 bits 381 against 402); row blocks that share them leave
 // them in the caches.  Waves a SIMD: what the registers of each form leave room for (two blocks of 16
 // rows in d = 64 use 168 in 8 bits, and more would cost the third wave).
-template <int D, int CT, int RT, bool STREAM>
+template <int D, int CT, int RT, bool STREAM, bool WIN>
 __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT == 1 && CT != kFp32) ? 2 : 1) void paged_attn_kernel(PagedAttnArgs a) {
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, RB = S::RB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
@@ -377,7 +383,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
   __shared__ float lds_ml[kPagedWaves][RT * 16][2];
   const PagedArgs& p = a.c;
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 15, g4 = lane >> 4;
-  const PagedPart part = paged_find<BK>(a, uniform((int)block_id()), lane);
+  const PagedPart part = paged_find<BK, WIN>(a, uniform((int)block_id()), lane);
   if (!part.any) return;
   const int b = uniform(part.b), g = uniform(part.g), len = uniform(part.len), n_new = uniform(part.n_new);
   const int rows = n_new * p.G, row0 = uniform(part.rb) * (RT * 16);
@@ -393,6 +399,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
   bf16x8 qb[RT][D / 32];
   f32x4 qf[RT][D / 16];
   int lim[RT];                       // the row sees positions below
+  int low[RT];                       // and, in a window, from here on besides the first
   int every = kFarPos;               // positions below which every row of the block sees
 #pragma unroll
   for (int t = 0; t < RT; ++t) {
@@ -401,6 +408,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     const int rr = real ? r : row0, nr = a.by_group.quot(rr);
     const long long q_el = (((long long)b * p.Ln + nr) * p.Hq + (long long)g * p.G + a.by_group.rem(rr, nr)) * D;
     lim[t] = !real ? 0 : p.causal ? len - n_new + 1 + nr : len;
+    low[t] = len - n_new + nr - a.window + 1;
     if constexpr (CT == kFp32) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) qf[t][i] = *(const f32x4*)((const float*)a.q + q_el + 16 * i + 4 * g4);
@@ -431,7 +439,21 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
   const int32_t* chosen = a.page_idx ? a.page_idx + ((long long)b * p.Hkv + g) * a.top_k : nullptr;
   // Blocks behind the last row's own position are in no row's sight.
   const int sight = p.causal ? len - n_new + 1 + a.by_group.quot(min(rows - 1, row0 + RT * 16 - 1)) : len;
-  const int n_steps = (chosen ? part.last : min(part.last, (max(sight, 0) + BK - 1) / BK)) - part.first;
+  // A window: the groups of 16 keys that some row of the block sees are visited in the order of those that all rows
+  // see, the last ones, the ones at the window's beginning, and the first positions of the sequence.
+  int from = 0, near = 0, turn = 0, far = 0, all_low = 0, any_low = 0;   // first group, groups, first one visited; first positions' groups
+  if constexpr (WIN) {
+    const int last_nr = a.by_group.quot(min(rows - 1, row0 + RT * 16 - 1)), first_nr = a.by_group.quot(row0);
+    any_low = len - n_new + first_nr - a.window + 1;   // from here on some row sees, and from there on all do
+    all_low = any_low + last_nr - first_nr;
+    const int end = min(len, max(sight, 0));
+    far = (min(a.n_sinks, end) + 15) / 16;
+    from = max(max(any_low, 0) / 16, far);
+    near = max(0, (end + 15) / 16 - from);
+    turn = min(max((max(all_low, 0) + 15) / 16 - from, 0), max(near - 1, 0));
+  }
+  const int n_blocks = WIN ? ((near + far) * 16 + BK - 1) / BK : (max(sight, 0) + BK - 1) / BK;
+  const int n_steps = (chosen ? part.last : min(part.last, n_blocks)) - part.first;
   int at_page[H], at_pos[H];
   int bad = kFarPos;                 // the least position on a page outside the pool
   auto locate = [&](int i0) {
@@ -442,14 +464,31 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       at_pos[h] = kFarPos;
       if (i < n_steps) {
         const int key = (part.first + i) * BK + wave * S::KS + h * 16;   // among the keys to visit
-        int ord = key >> p.log2R;
-        if (chosen) ord = ord < a.top_k ? chosen[ord] : -1;
-        const int pos = (int)((unsigned)ord << p.log2R) + (key & (p.R - 1));
-        if ((unsigned)ord < (unsigned)p.max_pages && pos < len) {
-          const int page = table[ord];
-          at_pos[h] = pos;
-          if ((unsigned)page < (unsigned)p.n_pages) at_page[h] = page;
-          else bad = min(bad, pos);
+        if constexpr (WIN) {
+          int group = key >> 4;
+          if (group < near) {
+            group += turn;
+            group = from + (group < near ? group : group - near);
+          } else {
+            group -= near;
+            group = group < far ? group : kFarPos / 16;
+          }
+          const int pos = group * 16;
+          if (pos < len) {
+            const int page = table[pos >> p.log2R];
+            at_pos[h] = pos;
+            at_page[h] = (unsigned)page < (unsigned)p.n_pages ? page : -1;
+          }
+        } else {
+          int ord = key >> p.log2R;
+          if (chosen) ord = ord < a.top_k ? chosen[ord] : -1;
+          const int pos = (int)((unsigned)ord << p.log2R) + (key & (p.R - 1));
+          if ((unsigned)ord < (unsigned)p.max_pages && pos < len) {
+            const int page = table[ord];
+            at_pos[h] = pos;
+            if ((unsigned)page < (unsigned)p.n_pages) at_page[h] = page;
+            else bad = min(bad, pos);
+          }
         }
       }
     }
@@ -460,7 +499,11 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     long long rows_at[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-      const int page = __builtin_amdgcn_readlane(at_page[h], i & 63);
+      int page = __builtin_amdgcn_readlane(at_page[h], i & 63);
+      if constexpr (WIN) {
+        s.bad[h] = page < 0;
+        page = max(page, 0);
+      }
       s.pos[h] = __builtin_amdgcn_readlane(at_pos[h], i & 63);
       const long long row = ((long long)page * p.Hkv + g) * page_rows + (s.pos[h] & (p.R - 1));
       const char* kp = (const char*)p.k_pages + row * RB + n * RB + (RB < 64 ? RB / 4 : 16) * g4;
@@ -513,6 +556,15 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       s.ex = *(const uint32_t*)((n & 2 ? p.v_exp : p.k_exp) + (n & 1 ? rows_at[H - 1] : rows_at[0]) + 4 * g4);
   };
 
+  // Whether row tile t, or any row of the block, sees a position.
+  auto sees = [&](int t, int pos) {
+    if constexpr (WIN) return pos < lim[t] && (pos >= low[t] || pos < a.n_sinks);
+    else return pos < lim[t];
+  };
+  auto in_sight = [&](int pos) {
+    if constexpr (WIN) return pos < len && (pos >= any_low || pos < a.n_sinks);
+    else return pos < len;
+  };
   // whole: every row sees every key of the step.
   auto compute = [&](PagedStep<D, CT>& s, auto whole_step) {
     constexpr bool whole = decltype(whole_step)::value;
@@ -556,7 +608,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     if constexpr (!whole) {
 #pragma unroll
       for (int j = 0; j < VR; ++j) {
-        const bool there = s.pos[j / 4] + 4 * g4 + j % 4 < len;
+        const bool there = in_sight(s.pos[j / 4] + 4 * g4 + j % 4);
 #pragma unroll
         for (int w = 0; w < W; ++w) v[j][w] = there ? v[j][w] : 0u;
       }
@@ -566,7 +618,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     // zeros in the products, and are added by themselves to the rows that see them, from a
     // copy of the step's values in the wave's part of lds_o.
     bool any_odd = false;
-    if (!whole && p.causal && n_new > 1) {
+    if (!whole && (WIN || p.causal) && n_new > 1) {
       float z = 0.f;
 #pragma unroll
       for (int j = 0; j < VR; ++j)
@@ -640,7 +692,8 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
         for (int e = 0; e < 4; ++e) {
           float x = sc[h][e] * p.scale_log2;
           if constexpr (CT == kFp8) x *= exp_to_scale((ke[h] >> (8 * e)) & 255);
-          if (!whole) x = s.pos[h] + 4 * g4 + e < lim[t] ? x : -INFINITY;
+          if (WIN && !whole) x = s.bad[h] ? NAN : x;   // the rows that see it, and no others
+          if (!whole) x = sees(t, s.pos[h] + 4 * g4 + e) ? x : -INFINITY;
           sc[h][e] = x;
           top = fmaxf(top, x);
         }
@@ -663,7 +716,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           l[t] += x;
           if constexpr (CT == kFp8) {
             x *= exp_to_scale((ve[h] >> (8 * e)) & 255);
-            if (!whole) x = s.pos[h] + 4 * g4 + e < lim[t] ? x : 0.f;   // bytes that no row wrote
+            if (!whole) x = sees(t, s.pos[h] + 4 * g4 + e) ? x : 0.f;   // bytes that no row wrote
           }
           pr[h][e] = x;
         }
@@ -713,7 +766,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
 #pragma unroll
           for (int i = 1; i < 4 * H; ++i) w = (key >> 4) * 4 + key % 4 == i ? pr[i / 4][i % 4] : w;
           w = __shfl(w, 16 * (key / 4 % 4) + n);
-          if ((key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16 >= lim[t]) continue;
+          if (!sees(t, (key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16)) continue;
           const uint32_t* copy = (const uint32_t*)&lds_o[wave][0][0] + key * (CT == kFp32 ? D : D / 2);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
@@ -739,7 +792,11 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     auto whole_before_another = [&]() {
       bool w = i + 1 < n_steps;
 #pragma unroll
-      for (int h = 0; h < H; ++h) w = w && __builtin_amdgcn_readlane(at_pos[h], i & 63) + 16 <= every;
+      for (int h = 0; h < H; ++h) {
+        const int pos = __builtin_amdgcn_readlane(at_pos[h], i & 63);
+        w = w && pos + 16 <= every;
+        if constexpr (WIN) w = w && (pos >= all_low || pos + 16 <= a.n_sinks) && __builtin_amdgcn_readlane(at_page[h], i & 63) >= 0;
+      }
       return w;
     };
     auto fetch_next = [&](PagedStep<D, CT>& s) {
@@ -922,18 +979,18 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a) {
   if (c == 0 && a.lse) a.lse[((long long)b * p.Hq + head) * p.Ln + nr] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
 }
 
-template <int D, int CT>
+template <int D, int CT, bool WIN>
 hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   const dim3 grid = grid_xy(a.grid);
   const int rows = a.c.G * a.c.Ln;
   if (a.plan) {
-    hipLaunchKernelGGL((paged_plan_kernel<PagedShape<D, CT>::BK>), dim3(1), dim3(1024), 0, s, a);
+    hipLaunchKernelGGL((paged_plan_kernel<PagedShape<D, CT>::BK, WIN>), dim3(1), dim3(1024), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1, true>), grid, dim3(256), 0, s, a);
-  else if (rows <= kPagedRows) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, false>), grid, dim3(256), 0, s, a);
+  if (rows <= 16) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 1, true, WIN>), grid, dim3(256), 0, s, a);
+  else if (rows <= kPagedRows) hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, true, WIN>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_attn_kernel<D, CT, 2, false, WIN>), grid, dim3(256), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.max_chunks == 1) return e;
   const long long all = (long long)a.c.B * a.c.Hkv * rows;
@@ -942,14 +999,19 @@ hipError_t paged_attn_of(const PagedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
+template <bool WIN>
+hipError_t attn_by_type(const PagedAttnArgs& a, hipStream_t s) {
   const bool wide = a.c.D == 128;
   switch (cache_type(a.c)) {
-    case kBf16: return wide ? paged_attn_of<128, kBf16>(a, s) : paged_attn_of<64, kBf16>(a, s);
-    case kFp8: return wide ? paged_attn_of<128, kFp8>(a, s) : paged_attn_of<64, kFp8>(a, s);
-    case kFp4: return wide ? paged_attn_of<128, kFp4>(a, s) : paged_attn_of<64, kFp4>(a, s);
-    default: return wide ? paged_attn_of<128, kFp32>(a, s) : paged_attn_of<64, kFp32>(a, s);
+    case kBf16: return wide ? paged_attn_of<128, kBf16, WIN>(a, s) : paged_attn_of<64, kBf16, WIN>(a, s);
+    case kFp8: return wide ? paged_attn_of<128, kFp8, WIN>(a, s) : paged_attn_of<64, kFp8, WIN>(a, s);
+    case kFp4: return wide ? paged_attn_of<128, kFp4, WIN>(a, s) : paged_attn_of<64, kFp4, WIN>(a, s);
+    default: return wide ? paged_attn_of<128, kFp32, WIN>(a, s) : paged_attn_of<64, kFp32, WIN>(a, s);
   }
+}
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
+  return a.window > 0 ? attn_by_type<true>(a, s) : attn_by_type<false>(a, s);
 }
 
 }  // namespace pd

@@ -84,12 +84,19 @@ hipError_t launch_paged_select(const PageSelectArgs& a, hipStream_t s);
 // Rows of one query block: the query rows of a (sequence, KV head) are taken in
 // blocks of at most this many.
 constexpr int kPagedRows = 32;
+// Keys that a block of query rows visits at most within a window: the first positions and the window of its first
+// row, each in groups of 16, and what the block's other rows see further (causal = 0: besides the new rows).
+inline long long paged_window_keys(long long window, long long n_sinks, long long rows_of_block) {
+  return (n_sinks + 15) / 16 * 16 + window + rows_of_block + 31;
+}
 
 struct PagedAttnArgs {
   PagedArgs c;
   const void* q;
   const int32_t* page_idx;  // nullptr: all pages
   int top_k;
+  int window, n_sinks;   // 0: no window
+  int window_keys;       // keys, in groups of 16, that a row block visits at most (causal = 0: and the new rows)
   void* o;
   float* lse;
   float* o_part;         // [slot][part_rows][D] sums of a workgroup whose keys are a part of its rows'
