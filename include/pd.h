@@ -408,6 +408,32 @@ pd_status pd_paged_append(const pd_paged_dims *dims, const pd_paged_cache *cache
                           int64_t k_stride, const void *v_new, int64_t v_stride, void *stream);
 
 /*
+ * pd_paged_append of rows as a projection gives them, with what pd_qk_norm_rope does
+ * to query and key rows on the way: new row r < new_rows[b] of sequence b is normed
+ * (w_q, w_k; NULL: not) and turned by its position, pos[b][r] or, with pos NULL, its
+ * position in the sequence kv_len[b] - new_rows[b] + r; the query row is written to
+ * q_out, the key row and the value row as it is into the pages.  Formulas, pairs and
+ * frequencies are pd_qk_norm_rope's; rope_base = 0: no rotation.  Norm and rotation are
+ * evaluated in double precision, the result is rounded to fp32 and then to dtype, and from
+ * there the pages and k_bounds hold what pd_paged_append makes of the rows, to the bit.
+ * (pd_qk_norm_rope works in fp32: an element of its results may differ by one
+ * rounding.)  With eps = 0 a head of zeros gives NaN; one with an infinity gives NaN in
+ * its place, and zeros elsewhere before the rotation.
+ * q, k_new, v_new (dtype): row (b, r) holds its heads of d contiguous elements at element
+ *   (b * L_n + r) * stride (each its own: all may point into the rows of a fused
+ *   projection).  w_q, w_k [d].  pos int32 [B][L_n], any values, or NULL.
+ * q_out [B][L_n][H_q][d] (dtype), as pd_paged_attn takes it: every row r < new_rows[b] is
+ *   written, those whose position in the sequence lies below 0 too, and others are left as they
+ *   were.  It may be q itself where q_stride = H_q * d; other overlaps of inputs and outputs are
+ *   not allowed.  q and q_out both NULL: keys and values alone.
+ * Strides: >= heads * d, multiples of 16 bytes.  eps >= 0 and rope_base >= 0 finite.  No workspace.
+ */
+pd_status pd_paged_append_rope(const pd_paged_dims *dims, const pd_paged_cache *cache, const void *q,
+                               int64_t q_stride, const void *k_new, int64_t k_stride, const void *v_new,
+                               int64_t v_stride, const void *w_q, const void *w_k, float eps, const int32_t *pos,
+                               double rope_base, void *q_out, void *stream);
+
+/*
  * Reads rows back: k_out, v_out [B][H_kv][n_rows][d] (dtype) receive positions
  * first..first+n_rows-1 of every sequence, dequantised; this is the prefix
  * layout of pd_sparse_decode_attn_compact.  Rows of positions >= kv_len[b] are

@@ -23,7 +23,7 @@ EXPORTS = ["pd_prefill_chunks", "pd_score_select", "pd_sparse_decode_attn", "pd_
            "pd_sparse_decode_attn_compact", "pd_compact_workspace_bytes", "pd_select_ranked",
            "pd_gather_joint", "pd_score_select_noalloc", "pd_qk_norm_rope", "pd_paged_append", "pd_paged_read",
            "pd_paged_select", "pd_paged_attn", "pd_paged_workspace_bytes", "pd_paged_window_attn",
-           "pd_paged_window_workspace_bytes"]
+           "pd_paged_window_workspace_bytes", "pd_paged_append_rope"]
 
 
 class PdError(RuntimeError):
@@ -147,6 +147,8 @@ def load(path: str = LIB_PATH):
     lib.pd_paged_select.restype = ctypes.c_int
     lib.pd_paged_attn.argtypes = [pp, cp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.pd_paged_attn.restype = ctypes.c_int
+    lib.pd_paged_append_rope.argtypes = [pp, cp, vp, i64, vp, i64, vp, i64, vp, vp, ctypes.c_float, vp, ctypes.c_double, vp, vp]
+    lib.pd_paged_append_rope.restype = ctypes.c_int
     lib.pd_paged_window_attn.argtypes = [pp, cp, vp, i32, i32, vp, vp, vp, sz, vp]
     lib.pd_paged_window_attn.restype = ctypes.c_int
     lib.pd_paged_window_workspace_bytes.argtypes = [pp, i32, i32]
@@ -449,6 +451,29 @@ def pd_paged_append(dims: PagedDims, cache: PagedCache, k_new, v_new, stream=Non
     kp, ks = _rows("k_new", k_new, shape, cache.type, dev)
     vp, vs = _rows("v_new", v_new, shape, cache.type, dev)
     _check(load().pd_paged_append(ctypes.byref(dims), c, kp, ks, vp, vs, _launch_stream(stream, dev)))
+
+
+def pd_paged_append_rope(dims: PagedDims, cache: PagedCache, q, k_new, v_new, w_q, w_k, eps, pos, rope_base, q_out,
+                         stream=None):
+    """Rows of a projection into the pages with head norms and rotary positions on the way (see include/pd.h): q
+    [B, L_n, H_q, d] into q_out, k_new, v_new [B, L_n, H_kv, d] into the pages; rows may be strided; q and q_out None: keys
+    and values alone; w_q, w_k None: no norm; pos [B, L_n] or None: the positions in the sequences; rope_base 0: no rotation."""
+    c, dev, d = cache._for(dims), cache.device, dims.head_dim
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    B, L = dims.batch, dims.new_len
+    shape, qp, qs, op = (B, L, dims.n_heads_kv, d), None, 0, None
+    if q is not None:
+        q_shape = (B, L, dims.n_heads_q, d)
+        qp, qs = _rows("q", q, q_shape, cache.type, dev)
+        op = _checked("q_out", q_out, q_shape, cache.type, dev)
+    kp, ks = _rows("k_new", k_new, shape, cache.type, dev)
+    vp, vs = _rows("v_new", v_new, shape, cache.type, dev)
+    wq = None if w_q is None else _checked("w_q", w_q, (d,), cache.type, dev)
+    wk = None if w_k is None else _checked("w_k", w_k, (d,), cache.type, dev)
+    pp = None if pos is None else _checked("pos", pos, (B, L), _KINDS["int32"], dev)
+    _check(load().pd_paged_append_rope(ctypes.byref(dims), c, qp, qs, kp, ks, vp, vs, wq, wk, eps, pp, rope_base, op,
+                                       _launch_stream(stream, dev)))
 
 
 def pd_paged_read(dims: PagedDims, cache: PagedCache, first, n_rows, k_out, v_out, stream=None):

@@ -145,80 +145,6 @@ hipError_t launch_qk_norm_rope(const NormRopeArgs& a, hipStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// What a lane needs to write its 16 bytes of rows into a page: row `base` of the pool is the page's
-// row 0 (of one KV head), c the lane of a row.
-template <int CT, int D>
-struct CacheRow {
-  static constexpr int E = CT == kFp32 ? 4 : 8, L = D / E, EB = CT == kFp32 ? 4 : 2;
-  char* dst;
-  uint8_t* ex;
-  int c;
-  __device__ __forceinline__ CacheRow(const PagedArgs& p, int kv, long long base, int lane) : ex(nullptr), c(lane) {
-    char* pages = (char*)(kv ? p.v_pages : p.k_pages);
-    uint8_t* exps = kv ? p.v_exp : p.k_exp;
-    if constexpr (CT == kFp4) {
-      dst = pages + base * (D / 2) + c * 4;
-      ex = exps + base * (D / 32) + (c / 4) * p.R;   // exponent bytes of 32 channels lie by rows
-    } else if constexpr (CT == kFp8) {
-      dst = pages + base * D + c * 8;
-      ex = exps + base;
-    } else {
-      dst = pages + base * (D * EB) + c * 16;
-    }
-  }
-  // Writes row `slot` of the page, where `live`; x: the lane's 16 bytes, y: their elements.  All
-  // lanes of a row are active.
-  __device__ __forceinline__ void put(const Row16<CT != kFp32>& x, const float* y, int slot, bool live) const {
-    if constexpr (CT == kFp8 || CT == kFp4) {
-      float m = 0.f;
-      bool finite = true;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float t = fabsf(y[e]);
-        finite = finite && t < INFINITY;
-        m = fmaxf(m, t < INFINITY ? t : 0.f);
-      }
-      if constexpr (CT == kFp8) {
-        m = lanes_max<L>(m);
-        const uint32_t bits = __float_as_uint(m);
-        const int e2 = min(max((int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0), -100), 120);
-        const float inv = __uint_as_float((uint32_t)(127 - e2) << 23);
-        uint32_t w[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          float z[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            z[e] = y[4 * k + e] * inv;
-            z[e] = fabsf(y[4 * k + e]) < INFINITY ? z[e] : NAN;
-          }
-          int v = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
-          w[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], v, true);
-        }
-        if (live) {
-          *(u32x2*)(dst + (long long)slot * D) = u32x2{w[0], w[1]};
-          if (c == 0) ex[slot] = (uint8_t)(e2 + 127);
-        }
-      } else {
-        // The group's four lanes: its maximum, or infinity where an element is not finite.
-        m = finite ? m : INFINITY;
-        m = fmaxf(m, dpp<0xb1>(m, m));
-        m = fmaxf(m, dpp<0x4e>(m, m));
-        const uint32_t bits = __float_as_uint(m);
-        const int e2 = min(max((int)(bits >> 23) - 129 + ((bits & 0x7fffffu) > 0x400000u ? 1 : 0), -100), 126);
-        const uint32_t w = to_fp4(y, exp_to_scale((uint32_t)(e2 + 127)));
-        if (live) {
-          *(uint32_t*)(dst + (long long)slot * (D / 2)) = w;
-          if ((c & 3) == 0) ex[slot] = m < INFINITY ? (uint8_t)(e2 + 127) : (uint8_t)255;
-        }
-      }
-    } else {
-      if (live) x.store_once(dst + (long long)slot * (D * EB));
-    }
-  }
-};
-
-// ---------------------------------------------------------------------------
 // Writing rows into the pages.
 //
 // One workgroup per (sequence, page that new rows fall into, KV head): the bounds of a
@@ -463,25 +389,6 @@ hipError_t launch_paged_read(const ReadArgs& a, hipStream_t s) {
 // and converted once; memory bounds it for few query rows (16 lanes or more read a
 // page's bounds in whole lines, a lane four pages at once: 512 pages of 8 x 32 heads 12.9 us,
 // one page at a time 18.7), the double FMAs (one per element and row) for many.
-
-// x + the same of the lane that `ctrl` names.
-template <int CTRL>
-__device__ __forceinline__ double add_dpp(double x) {
-  const u32x2 w = __builtin_bit_cast(u32x2, x);
-  const u32x2 y = {(uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[0], CTRL, 0xf, 0xf, true),
-                   (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[1], CTRL, 0xf, 0xf, true)};
-  return x + __builtin_bit_cast(double, y);
-}
-// Sum over groups of L neighbouring lanes, the same bits in each.
-template <int L>
-__device__ __forceinline__ double lanes_sum(double x) {
-  x = add_dpp<0xb1>(x);                            // quad_perm [1,0,3,2]
-  x = add_dpp<0x4e>(x);                            // quad_perm [2,3,0,1]
-  x = add_dpp<0x141>(x);                           // row_half_mirror
-  if constexpr (L >= 16) x = add_dpp<0x140>(x);    // row_mirror
-  if constexpr (L >= 32) x += __shfl_xor(x, 16);
-  return x;
-}
 
 constexpr int kScoreTurns = 4;   // pages of a lane
 constexpr int kScoreRows = 16;   // query rows in LDS at a time

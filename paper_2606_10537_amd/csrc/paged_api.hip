@@ -70,6 +70,13 @@ pd_status check_cache(const pd_paged_dims* d, const pd_paged_cache* c, bool page
   return PD_OK;
 }
 
+pd_status check_norm(float eps, double rope_base) {
+  if (!std::isfinite(eps) || eps < 0.f) return fail(PD_ERR_BAD_DIMS, "eps must be finite and >= 0");
+  if (!std::isfinite(rope_base) || rope_base < 0.0)
+    return fail(PD_ERR_BAD_DIMS, "rope_base must be finite and >= 0 (0: no rotation)");
+  return PD_OK;
+}
+
 pd_status check_stride(const char* name, int64_t stride, long long least, int elem) {
   if (stride < least || stride % (16 / elem) != 0 || stride > (1LL << 40))
     return fail(PD_ERR_BAD_DIMS, "%s=%lld must be at least %lld, a multiple of 16 bytes and at most 2^40", name,
@@ -246,9 +253,7 @@ pd_status pd_qk_norm_rope(int32_t n_rows, int32_t n_heads_q, int32_t n_heads_kv,
   if (head_dim != 64 && head_dim != 128) return fail(PD_ERR_UNSUPPORTED, "head_dim=%d must be 64 or 128", head_dim);
   if (dtype != PD_BF16 && dtype != PD_FP32)
     return fail(PD_ERR_UNSUPPORTED, "dtype=%d is neither PD_BF16 nor PD_FP32", dtype);
-  if (!std::isfinite(eps) || eps < 0.f) return fail(PD_ERR_BAD_DIMS, "eps must be finite and >= 0");
-  if (!std::isfinite(rope_base) || rope_base < 0.0)
-    return fail(PD_ERR_BAD_DIMS, "rope_base must be finite and >= 0 (0: no rotation)");
+  PD_RETURN_IF(check_norm(eps, rope_base));
   // A wave takes at least two heads (fp32, d = 128).
   if ((double)n_rows * ((n_heads_q + (long long)n_heads_kv + 1) / 2) >= 2147483640.0)
     return fail(PD_ERR_BAD_DIMS, "n_rows=%d rows of %lld heads are too large for one launch", n_rows,
@@ -315,6 +320,58 @@ pd_status pd_paged_append(const pd_paged_dims* d, const pd_paged_cache* cache, c
   a.by_heads = pd::fast_div(a.c.Hkv);
   a.by_pages = pd::fast_div(a.pages);
   return hip_status(pd::launch_paged_append(a, (hipStream_t)stream), "append kernel");
+}
+
+pd_status pd_paged_append_rope(const pd_paged_dims* d, const pd_paged_cache* cache, const void* q, int64_t q_stride,
+                               const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                               const void* w_q, const void* w_k, float eps, const int32_t* pos, double rope_base,
+                               void* q_out, void* stream) {
+  PD_RETURN_IF(check_paged_dims(d));
+  PD_RETURN_IF(check_norm(eps, rope_base));
+  PD_RETURN_IF(check_cache(d, cache, true, false));
+  PD_REQUIRE_PTR(k_new);
+  PD_REQUIRE_PTR(v_new);
+  const int eb = d->dtype == PD_BF16 ? 2 : 4;
+  const long long row = (long long)d->n_heads_kv * d->head_dim, q_row = (long long)d->n_heads_q * d->head_dim;
+  if (q || q_out) {
+    PD_REQUIRE_PTR(q);
+    PD_REQUIRE_PTR(q_out);
+    PD_RETURN_IF(check_stride("q_stride", q_stride, q_row, eb));
+    if (q == q_out && q_stride != q_row)
+      return fail(PD_ERR_BAD_DIMS, "q_out may be q only where its rows lie without gaps, q_stride=%lld", (long long)q_stride);
+  }
+  PD_RETURN_IF(check_stride("k_stride", k_stride, row, eb));
+  PD_RETURN_IF(check_stride("v_stride", v_stride, row, eb));
+  if (w_q && !aligned16(w_q)) return fail(PD_ERR_MISALIGNED, "pointer 'w_q' is not 16-byte aligned");
+  if (w_k && !aligned16(w_k)) return fail(PD_ERR_MISALIGNED, "pointer 'w_k' is not 16-byte aligned");
+  if (pos && !aligned16(pos)) return fail(PD_ERR_MISALIGNED, "pointer 'pos' is not 16-byte aligned");
+  // A workgroup takes at least four of the heads of a page's rows.
+  const long long chunks = ((q ? d->n_heads_q : 0) + 2LL * d->n_heads_kv + 3) / 4;
+  if ((double)d->batch * (double)chunks * touched_pages(d) >= (double)kMaxGrid)
+    return fail(PD_ERR_BAD_DIMS, "append of batch=%d with new_len=%d is too large for one launch", d->batch,
+                d->new_len);
+  pd::AppendRopeArgs a{};
+  a.c = paged_args(d, cache);
+  if (!q) a.c.Hq = 0;
+  a.q = q;
+  a.k = k_new;
+  a.v = v_new;
+  a.qs = q_stride;
+  a.ks = k_stride;
+  a.vs = v_stride;
+  a.w_q = w_q;
+  a.w_k = w_k;
+  a.q_out = q_out;
+  a.pos = pos;
+  a.eps = eps;
+  a.rotate = rope_base > 0.0;
+  if (a.rotate) {
+    const long double step = std::log2((long double)rope_base) * 2 / d->head_dim;
+    a.step = (double)(float)step;
+    a.step_rest = (double)(step - (long double)a.step);
+  }
+  a.pages = (int)touched_pages(d);
+  return hip_status(pd::launch_paged_append_rope(a, (hipStream_t)stream), "append kernel with norms and rotation");
 }
 
 pd_status pd_paged_read(const pd_paged_dims* d, const pd_paged_cache* cache, int32_t first, int32_t n_rows,

@@ -60,6 +60,24 @@ struct AppendArgs {
 };
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
 
+// Heads of the query, key and value rows that one workgroup takes, at most.
+constexpr int kRopeHeads = 16;
+struct AppendRopeArgs {
+  PagedArgs c;           // Hq = 0: no query rows
+  const void *q, *k, *v;
+  long long qs, ks, vs;  // row strides, elements
+  const void *w_q, *w_k; // norm weights or nullptr
+  void* q_out;
+  const int32_t* pos;    // nullptr: the positions in the sequences
+  float eps;
+  bool rotate;
+  double step, step_rest;  // log2(rope_base) * 2 / d in two parts, the first of 24 bits: pair i turns by pos * 2^(-i * step)
+  int pages;             // pages that the new rows of one sequence can touch
+  int heads;             // of a workgroup
+  FastDiv by_chunks, by_pages;
+};
+hipError_t launch_paged_append_rope(AppendRopeArgs a, hipStream_t s);
+
 struct ReadArgs {
   PagedArgs c;
   void *k_out, *v_out;

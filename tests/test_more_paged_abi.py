@@ -111,3 +111,54 @@ def test_binding_checks_window_calls(lib):  # noqa: F811
     other = dims(cache_dtype=PD_FP8_E4M3, n_pages=3, max_pages=2, page_rows=16)
     with pytest.raises(ValueError, match="differ"):
         _lib.pd_paged_window_attn(other, c, q, 4, 0, q)
+
+
+def rope(lib, d=None, c=None, q=A, qs=1024, k=A, ks=256, v=A, vs=256, wq=A, wk=A, eps=1e-6, pos=A, base=1e4, qo=A):
+    d, c = d or dims(), c or cache()
+    return lib.pd_paged_append_rope(ctypes.byref(d), ctypes.byref(c), q, qs, k, ks, v, vs, wq, wk, eps, pos, base, qo, None)
+
+
+@pytest.mark.parametrize("kw,want", BAD, ids=[str(k) for k, _ in BAD])
+def test_rope_sizes(lib, kw, want):  # noqa: F811
+    assert rope(lib, dims(**kw), qs=1 << 24, ks=1 << 24, vs=1 << 24) == want
+
+
+def test_rope_refusals(lib):  # noqa: F811
+    d, c = dims(), cache()
+    tail = (A, 1024, A, 256, A, 256, A, A, 1e-6, A, 1e4, A, None)
+    assert lib.pd_paged_append_rope(None, ctypes.byref(c), *tail) == NULL
+    assert lib.pd_paged_append_rope(ctypes.byref(d), None, *tail) == NULL
+    for name in ("k_pages", "v_pages", "page_table", "kv_len"):
+        assert rope(lib, c=cache(**{name: None})) == NULL and rope(lib, c=cache(**{name: MIS})) == ALIGN
+    for cache_dtype in (PD_FP8_E4M3, PD_FP4_E2M1):
+        for name in ("k_exp", "v_exp"):
+            assert rope(lib, dims(cache_dtype=cache_dtype), cache(**{name: None})) == NULL
+    assert rope(lib, c=cache(k_bounds=MIS)) == ALIGN and rope(lib, c=cache(new_rows=MIS)) == ALIGN
+    for name in ("q", "k", "v", "qo"):                          # q and q_out go together
+        assert rope(lib, **{name: None}) == NULL and rope(lib, **{name: MIS}) == ALIGN
+    for name in ("wq", "wk", "pos"):
+        assert rope(lib, **{name: MIS}) == ALIGN
+    assert rope(lib, eps=-1.0) == DIMS and rope(lib, eps=math.nan) == DIMS and rope(lib, eps=math.inf) == DIMS
+    assert rope(lib, base=-1.0) == DIMS and rope(lib, base=math.inf) == DIMS and rope(lib, base=math.nan) == DIMS
+    for name, least in (("qs", 1024), ("ks", 256), ("vs", 256)):
+        for bad in (least - 8, least + 4, (1 << 40) + 8, -(1 << 63)):
+            assert rope(lib, **{name: bad}) == DIMS
+    assert rope(lib, q=A, qo=A, qs=1032) == DIMS                 # in place, with gaps between the rows
+    assert b"q_out" in lib.pd_last_error_message()
+    huge = dims(batch=65536, n_heads_q=16384, n_heads_kv=16384, new_len=2, max_pages=1 << 24)
+    assert rope(lib, huge, qs=1 << 21, ks=1 << 21, vs=1 << 21) == DIMS
+
+
+def test_binding_checks_rope_calls(lib):  # noqa: F811
+    d, c = four()
+    fused = fake(2, 1, 12, 128, dtype=torch.bfloat16)
+    good = dict(q=fused[:, :, :8], k_new=fused[:, :, 8:10], v_new=fused[:, :, 10:], w_q=fake(128, dtype=torch.bfloat16),
+                w_k=None, eps=0.0, pos=fake(2, 1, dtype=torch.int32), rope_base=1e4,
+                q_out=fake(2, 1, 8, 128, dtype=torch.bfloat16))
+    for kw, text in ((dict(q=None), "together"), (dict(q_out=None), "together"), (dict(k_new=fused[:, :, 8:9]), "shape"),
+                     (dict(v_new=fused[:, :, 10:].float()), "type"), (dict(w_q=fake(64, dtype=torch.bfloat16)), "shape"),
+                     (dict(w_k=fake(128, dtype=torch.float32)), "type"), (dict(pos=fake(2, dtype=torch.int32)), "shape"),
+                     (dict(pos=fake(2, 1, dtype=torch.int64)), "type"), (dict(q_out=fused[:, :, :8].expand(2, 1, 8, 128)[..., :64]), "shape"),
+                     (dict(k_new=fused[:, :, 8:12:2]), "contiguous"), (dict(w_q=torch.zeros(128, dtype=torch.bfloat16)), "GPU")):
+        with pytest.raises(ValueError, match=text):
+            _lib.pd_paged_append_rope(d, c, **dict(good, **kw))
