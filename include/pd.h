@@ -483,7 +483,7 @@ pd_status pd_paged_select(const pd_paged_dims *dims, const pd_paged_cache *cache
  * and no others.
  * With dtype = PD_BF16 the weights multiply V as two bf16 terms (15 bits) where a
  * KV head has at most 16 query rows, G * L_n <= 16, and rounded to bf16 where it has
- * more (their sum, and so lse, is taken before); sums are fp32 and divided at the
+ * more or the pages are PD_FP4_E2M1 (their sum, and so lse, is taken before); sums are fp32 and divided at the
  * end, so they overflow where 256 * sum |v| over the visible keys passes 2^128.
  * A visible value that is infinite gives the infinity, or NaN where its weight
  * has underflowed (about 2^-126 of the row's largest); NaN gives NaN.

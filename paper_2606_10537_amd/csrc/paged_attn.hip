@@ -14,7 +14,8 @@
 //   evenly; rows whose keys are cut are joined by a second kernel.
 //
 // Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
-// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; 64 ragged sequences of up to
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; in 4 bits 209 us, 5.5 TB/s (its loads
+// alone 170, its arithmetic alone 172: conversions and the matrix products of one row in 16); 64 ragged sequences of up to
 // 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s (its loads bound it: 368 us with the arithmetic
 // of the whole steps left out, 215 with their loads left out).  One token of one 8K sequence takes 7.2 +
 // 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
@@ -318,7 +319,7 @@ struct PagedShape {
   static constexpr int NT = D / 16;                         // products of P V
   // First channel of result row m (all but fp32).
   static __device__ __forceinline__ int base(int m) {
-    return CT == kFp8 || (CT == kFp4 && D == 64) ? 2 * E * (m & 7) + E * (m >> 3) : E * m;
+    return CT == kFp8 ? 2 * E * (m & 7) + E * (m >> 3) : CT == kFp4 ? D / 4 * (m & 3) + E * (m >> 2) : E * m;
   }
   static constexpr int BK = kPagedWaves * KS;
 };
@@ -328,9 +329,8 @@ template <int D, int CT>
 struct PagedStep {
   using S = PagedShape<D, CT>;
   u32x4 k[S::H][S::NK];
-  uint32_t v[S::VR][S::VW];      // E4M3: read 2 j + i of 16 keys, rows 2 j and 2 j + 1 in a line
+  uint32_t v[S::VR][S::VW];      // E4M3: read 2 j + i of 16 keys, rows 2 j and 2 j + 1 in a line; E2M1: see load
   uint32_t ex;                   // exponent bytes of four keys (see load)
-  uint32_t kx[S::H], vx[S::H];   // 4 bits: exponent byte of the lane's K group, those of its V group of four keys
   int pos[S::H];                 // position of the first key of each 16
   bool bad[S::H];                // windows: their page lies outside the pool
 };
@@ -379,6 +379,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
   using S = PagedShape<D, CT>;
   constexpr int H = S::H, RB = S::RB, NK = S::NK, VR = S::VR, VW = S::VW, E = S::E, NT = S::NT, BK = S::BK;
   constexpr int OP = D + 4;
+  constexpr bool kTwo = RT == 1 && CT != kFp4;   // weights of two bf16 terms (see below)
   __shared__ float lds_o[kPagedWaves][16][OP];
   __shared__ float lds_ml[kPagedWaves][RT * 16][2];
   const PagedArgs& p = a.c;
@@ -495,6 +496,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
   };
 
   const uint32_t page_rows = (uint32_t)p.R;
+  const uint8_t* ex_lane = CT == kFp4 ? (n & 8 ? p.k_exp : p.v_exp) + (D == 64 ? (n & 3) / 2 : n & 3) * p.R + 4 * g4 : nullptr;
   auto load = [&](PagedStep<D, CT>& s, int i) {
     long long rows_at[H];
 #pragma unroll
@@ -516,12 +518,18 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       }
       const char* vp = (const char*)p.v_pages + row * RB + g4 * (4 * RB);
       if constexpr (CT == kFp4) {
-        // Eight neighbouring channels of four keys; in d = 64 lanes n and n ^ 8 read the same and keep four each.
-        const long long row_exp = (row - (s.pos[h] & (p.R - 1))) * (D / 32) + (s.pos[h] & (p.R - 1));
+        // The 16 rows in a line: lane n has a quarter (n % 4) of row 4 g + n / 4, and four lanes swap later.  Loads of
+        // 4 bytes, a row each, were four times as many (8 x 32 heads x 32K keys 277 us, now 230).
+        const char* at = (const char*)p.v_pages + row * RB;
+        if constexpr (D == 128) {
+          const u32x4 w = fetch<STREAM>((const u32x4*)(at + 16u * (uint32_t)lane));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s.v[4 * h + j][0] = fetch<STREAM>((const uint32_t*)(vp + j * RB) + (D == 64 ? n & 7 : n));
-        s.kx[h] = p.k_exp[row_exp + (long long)(D == 64 ? g4 >> 1 : g4) * p.R + n];
-        s.vx[h] = *(const uint32_t*)(p.v_exp + row_exp + (long long)(D == 64 ? (n & 7) >> 2 : n >> 2) * p.R + 4 * g4);
+          for (int j = 0; j < 4; ++j) s.v[4 * h + j][0] = w[j];
+        } else {
+          const u32x2 w = fetch<STREAM>((const u32x2*)(at + 8u * (uint32_t)lane));
+          s.v[4 * h][0] = w[0];
+          s.v[4 * h + 1][0] = w[1];
+        }
       } else if constexpr (CT == kFp8) {
         // Lanes n and n ^ 8 read twice the channels that they need, of two keys each, and swap
         // halves later: loads of 8 bytes a lane were twice as many (one sequence of 128K keys
@@ -552,6 +560,16 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     }
     // One load of all exponent bytes: keys 4 g.. of K's first 16 in lanes n = 0 (mod 4), of its
     // second in 1, of V's in 2 and 3.
+    // E2M1: four bytes of group n % 4 (d = 64: n % 4 / 2), keys 4 g.. of V's first 16 in lanes n / 4 = 0, of its
+    // second in 1, of K's in 2 and 3.
+    if constexpr (CT == kFp4) {
+      auto line = [&](int h) {
+        const int slot = s.pos[h] & (p.R - 1);
+        return (rows_at[h] - slot) * (D / 32) + slot;
+      };
+      const long long at0 = line(0), at1 = line(H - 1);
+      s.ex = *(const uint32_t*)(ex_lane + (n & 4 ? at1 : at0));
+    }
     if constexpr (CT == kFp8)
       s.ex = *(const uint32_t*)((n & 2 ? p.v_exp : p.k_exp) + (n & 1 ? rows_at[H - 1] : rows_at[0]) + 4 * g4);
   };
@@ -572,13 +590,36 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     // an infinity or a NaN.
     constexpr int W = CT == kFp32 ? VW : D / 32;
     uint32_t v[VR][W], ke[H], ve[H];
+    uint32_t y[VR];                  // E2M1: the lane's channels of its eight keys (d = 64: of two keys each)
+    float vs[VR];                    // and their powers of two
     if constexpr (CT == kFp4) {
 #pragma unroll
-      for (int j = 0; j < VR; ++j) {
-        const u32x4 x = from_fp4(D == 64 ? s.v[j][0] >> (2 * (n & 8)) : s.v[j][0], exp_to_scale((s.vx[j / 4] >> (8 * (j % 4))) & 255));
+      for (int h = 0; h < H; ++h) {
+        ke[h] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * (n >> 2) + 8 + 4 * h + g4), (int)s.ex) >> (8 * (n & 3)) & 255;
+        ve[h] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * (16 * g4 + 4 * h + (n & 3)), (int)s.ex);
+        // Lanes n, n ^ 4, n ^ 8, n ^ 12 hold the same quarter of four keys; each keeps its part of all four.
+        if constexpr (D == 128) {
+          uint32_t u[2], w[2];
 #pragma unroll
-        for (int w = 0; w < W; ++w) v[j][w] = x[w];
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t lo = s.v[4 * h + c][0], hi = s.v[4 * h + c + 2][0];
+            u[c] = dpp_bits<0x128, 0xc>(lo, hi);   // row_ror:8
+            w[c] = dpp_bits<0x128, 0x3>(hi, lo);
+          }
+          y[4 * h] = dpp_bits<0x114, 0xa>(u[0], u[1]);       // row_shr:4
+          y[4 * h + 1] = dpp_bits<0x104, 0x5>(u[1], u[0]);   // row_shl:4
+          y[4 * h + 2] = dpp_bits<0x114, 0xa>(w[0], w[1]);
+          y[4 * h + 3] = dpp_bits<0x104, 0x5>(w[1], w[0]);
+        } else {
+          const uint32_t lo = s.v[4 * h][0], hi = s.v[4 * h + 1][0];
+          const uint32_t u = dpp_bits<0x128, 0xc>(lo, hi), w = dpp_bits<0x128, 0x3>(hi, lo);
+          const uint32_t sel = n & 4 ? 0x03020706u : 0x05040100u;
+          y[4 * h] = __builtin_amdgcn_perm(dpp_bits<0x104, 0x5>(dpp_bits<0x114, 0xa>(u, u), u), u, sel);
+          y[4 * h + 2] = __builtin_amdgcn_perm(dpp_bits<0x104, 0x5>(dpp_bits<0x114, 0xa>(w, w), w), w, sel);
+        }
       }
+#pragma unroll
+      for (int j = 0; j < VR; ++j) vs[j] = exp_to_scale((ve[j / 4] >> (8 * (j % 4))) & 255);
     } else if constexpr (CT == kFp8) {
 #pragma unroll
       for (int h = 0; h < H; ++h) {
@@ -605,7 +646,16 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
 #pragma unroll
         for (int w = 0; w < W; ++w) v[j][w] = s.v[j][w];
     }
-    if constexpr (!whole) {
+    if constexpr (!whole && CT == kFp4) {
+#pragma unroll
+      for (int j = 0; j < VR; ++j) {
+        const bool there = in_sight(s.pos[j / 4] + 4 * g4 + j % 4);
+        vs[j] = there ? vs[j] : 1.f;
+        if constexpr (D == 128) y[j] = there ? y[j] : 0u;
+        else y[j & ~1] = there ? y[j & ~1] : y[j & ~1] & (j & 1 ? 0xffffu : 0xffff0000u);
+      }
+    }
+    if constexpr (!whole && CT != kFp4) {
 #pragma unroll
       for (int j = 0; j < VR; ++j) {
         const bool there = in_sight(s.pos[j / 4] + 4 * g4 + j % 4);
@@ -618,7 +668,26 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     // zeros in the products, and are added by themselves to the rows that see them, from a
     // copy of the step's values in the wave's part of lds_o.
     bool any_odd = false;
-    if (!whole && (WIN || p.causal) && n_new > 1) {
+    if (CT == kFp4 && !whole && (WIN || p.causal) && n_new > 1) {
+      // A key's group of channels is NaN or holds no such value: the copy has a word for each.
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < VR; ++j) odd = odd || !(vs[j] < INFINITY);
+      any_odd = __any(odd);
+      if (any_odd) {
+        uint32_t* copy = (uint32_t*)&lds_o[wave][0][0];   // [key of the step][quarter of the channels]
+#pragma unroll
+        for (int j = 0; j < VR; ++j) {
+          const bool nan = !(vs[j] < INFINITY);
+          copy[(16 * (j / 4) + 4 * g4 + j % 4) * 4 + (n & 3)] = nan ? kNanWord : 0u;
+          vs[j] = nan ? 1.f : vs[j];
+          if constexpr (D == 128) y[j] = nan ? 0u : y[j];
+          else y[j & ~1] = nan ? y[j & ~1] & (j & 1 ? 0xffffu : 0xffff0000u) : y[j & ~1];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
+    }
+    if (CT != kFp4 && !whole && (WIN || p.causal) && n_new > 1) {
       float z = 0.f;
 #pragma unroll
       for (int j = 0; j < VR; ++j)
@@ -669,7 +738,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
         } else if constexpr (CT == kFp4) {
 #pragma unroll
           for (int i = 0; i < D / 32; ++i)
-            sc[h] = mfma16x16x32(__builtin_bit_cast(bf16x8, from_fp4(s.k[h][0][i], exp_to_scale(s.kx[h]))), qb[t][i], sc[h]);
+            sc[h] = mfma16x16x32(__builtin_bit_cast(bf16x8, from_fp4(s.k[h][0][i], exp_to_scale(ke[h]))), qb[t][i], sc[h]);
         } else {
 #pragma unroll
           for (int i = 0; i < NK; ++i)
@@ -727,18 +796,29 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           for (int i = 0; i < NT; ++i)
             o[t][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j][i]), pr[0][j], o[t][i], 0, 0, 0);
       } else {
+        if constexpr (CT == kFp4) {
+          if (t == 0) {
+#pragma unroll
+            for (int j = 0; j < VR; ++j) {
+              const u32x4 x = from_fp4(D == 128 ? y[j] : y[j & ~1], vs[j]);
+#pragma unroll
+              for (int w = 0; w < W; ++w) v[j][w] = D == 128 || j % 2 == 0 ? x[w] : x[w + 2];
+            }
+          }
+        }
         // The weights as bf16; their sum l is taken before.  One tile of rows: two terms, the upper half of
         // the weight's bits and the rest rounded, 15 bits or more, so that the output's rounding is what is left
         // of the error (64 ragged requests in 8 bits 1.95e-3 of the 2-norm with weights of one term, 1.65e-3 with two);
         // memory bounds such calls, and the second product costs nothing there (8 x 32 heads x 32K keys 614.5 and
         // 615.1 us, one token of 8K keys 10.2 and 10.3).  Two tiles: one term, rounded to nearest; the second would be
         // paid for (32 rows of 4 heads over 8 x 8K keys 85.4 us with one, 89.1 with two; in 8 bits 84.4 and 97.9, d = 64
-        // 50.3 and 57.4).
+        // 50.3 and 57.4).  E2M1 values, whose own rounding is 2^-3 and more, take one term: their products do not hide
+        // behind the memory (8 x 32 heads x 32K keys 210 us with one term, 232 with two; 64 ragged requests 201 and 221).
         u32x4 pw, pl;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float x = pr[j < 2 ? 0 : H - 1][2 * (j & 1)], y = pr[j < 2 ? 0 : H - 1][2 * (j & 1) + 1];
-          if constexpr (RT == 1) {
+          if constexpr (kTwo) {
             const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
             pw[j] = __builtin_amdgcn_perm(b, a, 0x07060302u);
             // 2^-24 of the weight more: a second term of zero would turn infinite values into NaN
@@ -754,11 +834,23 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
 #pragma unroll
           for (int j = 0; j < 4; ++j)
             w[j] = __builtin_amdgcn_perm(v[2 * j + 1][i / 2], v[2 * j][i / 2], i & 1 ? 0x07060302u : 0x05040100u);
-          if constexpr (RT == 1) o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pl), o[t][i]);
+          if constexpr (kTwo) o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pl), o[t][i]);
           o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), o[t][i]);
         }
       }
-      if (!whole && any_odd) {
+      if (CT == kFp4 && !whole && any_odd) {
+#pragma unroll 1
+        for (int key = 0; key < S::KS; ++key) {
+          if (!sees(t, (key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16)) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float x = __uint_as_float(((const uint32_t*)&lds_o[wave][0][0])[key * 4 + r]);   // row 4 g + r is in quarter r
+#pragma unroll
+            for (int i = 0; i < NT; ++i) o[t][i][r] += x;
+          }
+        }
+      }
+      if (CT != kFp4 && !whole && any_odd) {
         for (int key = 0; key < S::KS; ++key) {
           // The row's weight of the key, from the lane that holds it: a value counts with its weight
           // as in a product, so where this has underflowed an infinity gives NaN here too.
@@ -793,9 +885,11 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       bool w = i + 1 < n_steps;
 #pragma unroll
       for (int h = 0; h < H; ++h) {
-        const int pos = __builtin_amdgcn_readlane(at_pos[h], i & 63);
-        w = w && pos + 16 <= every;
-        if constexpr (WIN) w = w && (pos >= all_low || pos + 16 <= a.n_sinks) && __builtin_amdgcn_readlane(at_page[h], i & 63) >= 0;
+        w = w && __builtin_amdgcn_readlane(at_pos[h], i & 63) + 16 <= every;
+        if constexpr (WIN) {
+          const int pos = __builtin_amdgcn_readlane(at_pos[h], i & 63);
+          w = w && (pos >= all_low || pos + 16 <= a.n_sinks) && __builtin_amdgcn_readlane(at_page[h], i & 63) >= 0;
+        }
       }
       return w;
     };
