@@ -110,6 +110,19 @@ __device__ __forceinline__ float lanes_sum(float x) {
   return x;
 }
 
+// The value of lane ^ L / 2 (partner).
+template <int L>
+__device__ __forceinline__ double partner(double x) {
+  const u32x2 w = __builtin_bit_cast(u32x2, x);
+  u32x2 y;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (L == 16) y[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w[i], 0x128, 0xf, 0xf, true);   // row_ror:8
+    else y[i] = __float_as_uint(partner<L>(__uint_as_float(w[i])));
+  }
+  return __builtin_bit_cast(double, y);
+}
+
 // x + the same of the lane that `ctrl` names.
 template <int CTRL>
 __device__ __forceinline__ double add_dpp(double x) {

@@ -61,7 +61,7 @@ struct AppendArgs {
 hipError_t launch_paged_append(const AppendArgs& a, hipStream_t s);
 
 // Heads of the query, key and value rows that one workgroup takes, at most.
-constexpr int kRopeHeads = 16;
+constexpr int kRopeHeads = 8;
 struct AppendRopeArgs {
   PagedArgs c;           // Hq = 0: no query rows
   const void *q, *k, *v;
@@ -70,7 +70,7 @@ struct AppendRopeArgs {
   void* q_out;
   const int32_t* pos;    // nullptr: the positions in the sequences
   float eps;
-  bool rotate;
+  bool rotate, stream;   // stream: query rows past the caches
   double step, step_rest;  // log2(rope_base) * 2 / d in two parts, the first of 24 bits: pair i turns by pos * 2^(-i * step)
   int pages;             // pages that the new rows of one sequence can touch
   int heads;             // of a workgroup
