@@ -15,7 +15,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libpd.so")
 SOURCES = ["pd_api.hip", "attn_bf16.hip", "attn_f32.hip", "select.hip", "diag.hip",
-           "paged_api.hip", "paged.hip", "paged_rope.hip", "paged_attn.hip"]
+           "paged_api.hip", "paged.hip", "paged_rope.hip", "paged_attn.hip",
+           "paged_tile.hip"]
 ARCH = "gfx950"
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -125,7 +125,8 @@ struct AttnPlan {
   size_t o_bytes, ml_bytes, unit_bytes, total;
   bool planned;
 };
-pd_status attn_plan(const pd_paged_dims* d, int top_k, long long most_keys, AttnPlan* p) {
+// whole: the keys of a unit are not cut.
+pd_status attn_plan(const pd_paged_dims* d, int top_k, long long most_keys, bool whole, AttnPlan* p) {
   const long long rows = (long long)(d->n_heads_q / d->n_heads_kv) * d->new_len;
   p->row_blocks = cdiv(rows, pd::kPagedRows);
   p->part_rows = (int)std::min<long long>(rows, pd::kPagedRows);
@@ -136,7 +137,7 @@ pd_status attn_plan(const pd_paged_dims* d, int top_k, long long most_keys, Attn
     return fail(PD_ERR_BAD_DIMS, "attention of batch=%d with new_len=%d is too large for one launch", d->batch,
                 d->new_len);
   p->parts = pd::paged_parts(rows);
-  p->max_chunks = blocks <= pd::paged_whole_blocks(units) ? 1 : (int)std::min<long long>(blocks, p->parts);
+  p->max_chunks = whole || blocks <= pd::paged_whole_blocks(units) ? 1 : (int)std::min<long long>(blocks, p->parts);
   // The kernels cut with a quota of at least all blocks / parts: at most so many whole
   // quotas, and one part that is not whole for each unit.
   p->grid = p->max_chunks == 1 ? units : std::min(units + p->parts, units * p->max_chunks);
@@ -183,6 +184,7 @@ pd_status check_attn_pages(const pd_paged_dims* d, const int32_t* page_idx, int 
 struct Window {
   int window, n_sinks, keys;   // keys: of a row block, see PagedAttnArgs
   long long most_keys;         // of any
+  int tile_rows;               // paged_tile_rows
 };
 pd_status check_window(int window, int n_sinks) {
   if (window < 1) return fail(PD_ERR_BAD_DIMS, "window=%d must be >= 1", window);
@@ -200,6 +202,9 @@ Window window_of(const pd_paged_dims* d, int window, int n_sinks) {
   const long long keys = pd::paged_window_keys(w.window, w.n_sinks, d->causal ? rows : 0);
   w.keys = (int)std::min<long long>(keys, kMaxPositions);
   w.most_keys = w.keys + (d->causal ? 0 : (long long)d->new_len);
+  // The tile kernel scales scores that it has masked with -inf: not where the scale may vanish in fp32.
+  if (!(d->sm_scale > 0.f) || d->sm_scale >= 1e-30f)
+    w.tile_rows = pd::paged_tile_rows(d->dtype == PD_BF16, (long long)d->batch * d->n_heads_kv, (long long)G * d->new_len);
   return w;
 }
 
@@ -207,7 +212,7 @@ pd_status launch_attn(const pd_paged_dims* d, const pd_paged_cache* cache, const
                       int top_k, const Window* w, void* o, float* lse, void* workspace, size_t ws_bytes,
                       void* stream) {
   AttnPlan plan;
-  PD_RETURN_IF(attn_plan(d, top_k, w ? w->most_keys : kMaxPositions, &plan));
+  PD_RETURN_IF(attn_plan(d, top_k, w ? w->most_keys : kMaxPositions, w && w->tile_rows, &plan));
   PD_RETURN_IF(check_ws(workspace, ws_bytes, plan.total));
   pd::PagedAttnArgs a{};
   a.c = paged_args(d, cache);
@@ -235,6 +240,7 @@ pd_status launch_attn(const pd_paged_dims* d, const pd_paged_cache* cache, const
   a.by_rows = pd::fast_div(a.c.G * a.c.Ln);
   a.by_blocks = pd::fast_div(a.row_blocks);
   a.by_units = pd::fast_div(a.c.Hkv * a.row_blocks);
+  if (w && w->tile_rows) return hip_status(pd::launch_paged_tile(a, w->tile_rows, (hipStream_t)stream), "paged attention kernel");
   return hip_status(pd::launch_paged_attn(a, (hipStream_t)stream), "paged attention kernels");
 }
 
@@ -449,13 +455,14 @@ size_t pd_paged_workspace_bytes(const pd_paged_dims* d, int32_t top_k, int32_t w
   if (which == 0) return check_select_dims(d, top_k) == PD_OK ? select_bytes(d) : 0;
   if (which != 1) return 0;
   AttnPlan plan;
-  return attn_plan(d, top_k, kMaxPositions, &plan) == PD_OK ? plan.total : 0;
+  return attn_plan(d, top_k, kMaxPositions, false, &plan) == PD_OK ? plan.total : 0;
 }
 
 size_t pd_paged_window_workspace_bytes(const pd_paged_dims* d, int32_t window, int32_t n_sinks) {
   if (check_paged_dims(d) != PD_OK || check_window(window, n_sinks) != PD_OK) return 0;
   AttnPlan plan;
-  return attn_plan(d, 0, window_of(d, window, n_sinks).most_keys, &plan) == PD_OK ? plan.total : 0;
+  const Window w = window_of(d, window, n_sinks);
+  return attn_plan(d, 0, w.most_keys, w.tile_rows > 0, &plan) == PD_OK ? plan.total : 0;
 }
 
 }  // extern "C"

@@ -146,5 +146,11 @@ constexpr int kPlanBatch = 128;
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+// Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does.
+inline int paged_tile_rows(bool bf16, long long pairs, long long rows) {
+  if (!bf16 || rows < 64 || pairs * ((rows + 63) / 64) < 64) return 0;
+  return pairs * ((rows + 127) / 128) >= 256 ? 128 : 64;
+}
+hipError_t launch_paged_tile(PagedAttnArgs a, int rows, hipStream_t s);
 
 }  // namespace pd
