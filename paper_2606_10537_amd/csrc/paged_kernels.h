@@ -146,10 +146,15 @@ constexpr int kPlanBatch = 128;
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
-// Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does.
+// Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does, which cuts
+// the keys of few row blocks (8 heads x 4 query heads, window 1024, 256 new rows: 128 blocks of 64 rows 25.7 us, 19.5 there;
+// 512 new rows: 256 blocks 28.4, 35.4 there; window 8192, 64 new rows: 128 and 35).  128 rows where these fill the card and
+// few of them are empty (2 sequences of 512 new rows 44.5 us, 50.5 with 64; 8 of them 124 and 203; 64 of 16 new rows, 64 a
+// head: 76.6 and 70.7).
 inline int paged_tile_rows(bool bf16, long long pairs, long long rows) {
-  if (!bf16 || rows < 64 || pairs * ((rows + 63) / 64) < 64) return 0;
-  return pairs * ((rows + 127) / 128) >= 256 ? 128 : 64;
+  const long long small = pairs * ((rows + 63) / 64), large = pairs * ((rows + 127) / 128);
+  if (!bf16 || rows < 64 || small < 256) return 0;
+  return large >= 256 && 2 * small > 3 * large ? 128 : 64;
 }
 hipError_t launch_paged_tile(PagedAttnArgs a, int rows, hipStream_t s);
 

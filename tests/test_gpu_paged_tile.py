@@ -10,7 +10,7 @@ import torch
 from paged_case import h64
 from paper_2606_10537_amd import _lib
 from paper_2606_10537_amd._lib import PD_BF16, PD_FP4_E2M1, PD_FP8_E4M3
-from test_gpu_paged_window import check, hide, make, run, run_window
+from test_gpu_paged_window import check, hide, make, run, run_window  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 KINDS = [(PD_BF16, PD_BF16), (PD_BF16, PD_FP8_E4M3), (PD_BF16, PD_FP4_E2M1)]
@@ -19,8 +19,8 @@ IDS = ["bf16", "fp8", "fp4"]
 
 @pytest.mark.parametrize("kind", KINDS, ids=IDS)
 @pytest.mark.parametrize("causal", [0, 1])
-@pytest.mark.parametrize("L,hq,hkv,d,R", [(64, 8, 8, 64, 16), (33, 16, 4, 128, 64), (130, 6, 3, 64, 32), (20, 28, 4, 128, 256),
-                                          (257, 2, 2, 128, 16)])
+@pytest.mark.parametrize("L,hq,hkv,d,R", [(64, 32, 32, 64, 16), (33, 32, 16, 128, 64), (130, 16, 8, 64, 32), (20, 84, 12, 128, 256),
+                                          (257, 8, 8, 128, 16)])
 def test_windows_and_first_positions(gpu_lib, kind, causal, L, hq, hkv, d, R):
     """Windows of one position, across a tile, across several and wider than the sequences; sequences of nothing but new
     rows, of few of them, without any."""
@@ -33,22 +33,22 @@ def test_windows_and_first_positions(gpu_lib, kind, causal, L, hq, hkv, d, R):
 @pytest.mark.parametrize("kind", KINDS, ids=IDS)
 def test_128_rows_a_workgroup(gpu_lib, kind):
     g = torch.Generator().manual_seed(1)
-    B, L = 20, 40
+    B, L = 8, 60
     lens = [int(x) for x in torch.randint(0, 400, (B,), generator=g)]
-    new = [min(L, n, int(x)) for n, x in zip(lens, torch.randint(0, 60, (B,), generator=g))]
+    new = [min(L, n, int(x)) for n, x in zip(lens, torch.randint(0, 90, (B,), generator=g))]
     for causal in (0, 1):
         for d in (64, 128):
-            run("128", kind, lens, 90, 4, new_len=L, new=new, hq=52, hkv=13, d=d, R=16, causal=causal, seed=d)
+            run("128", kind, lens, 90, 4, new_len=L, new=new, hq=64, hkv=16, d=d, R=16, causal=causal, seed=d)
 
 
 def test_more_than_sixteen_tiles(gpu_lib):
     """Windows of more than 1024 positions: where their groups lie is looked up again."""
     for window, sinks in ((2500, 130), (1 << 30, 0)):
-        run("long", KINDS[0], [3000, 1100, 2049, 90], window, sinks, new_len=64, hq=16, hkv=16, d=64, R=64, new=[64, 64, 64, 64], seed=3)
+        run("long", KINDS[0], [3000, 1100, 2049, 90], window, sinks, new_len=64, hq=64, hkv=64, d=64, R=64, new=[64, 9, 30, 64], seed=3)
 
 
 def test_the_same_bits_again_and_no_workspace(gpu_lib):
-    case, c, o, lse = run("again", KINDS[0], [700, 300, 500, 400], 200, 4, new_len=70, hq=16, hkv=8, d=128, R=16, seed=4)
+    case, c, o, lse = run("again", KINDS[0], [700, 300, 500, 400], 200, 4, new_len=70, hq=64, hkv=32, d=128, R=16, seed=4)
     assert _lib.pd_paged_window_workspace_bytes(case.dims, 200, 4) == 0
     again = run_window(case, c, 200, 4)
     assert torch.equal(o, again[0]) and torch.equal(lse, again[1])
@@ -63,12 +63,13 @@ def test_the_same_bits_again_and_no_workspace(gpu_lib):
 def test_nonfinite_rows_stay_with_the_rows_that_see_them(gpu_lib, kind, causal, which, d):
     """A NaN or an infinity at a position: the rows that do not see it keep their bits; the others get what the formula
     gives, also where all rows of a tile see it."""
-    L, W, n, hkv = 70, 30, 200, 64
+    L, W, n, hkv = 70, 30, 200, 128
     for bad in ((math.nan,) if kind[1] != PD_BF16 else (math.nan, math.inf, -math.inf)):
         for at in (1, 120, 150, 199):
             case = make(kind, [n], new_len=L, hq=hkv, hkv=hkv, d=d, R=16, causal=causal, seed=12)
             clean, _ = run_window(case, case.to_gpu(), W, 2)
-            check(case, clean, None, W, 2)
+            if at == 1 and (bad != bad) and which == "k":
+                check(case, clean, None, W, 2)
             rows = case.k_rows if which == "k" else case.v_rows
             ch = d - 5
             rows[0][at, 0, ch] = bad
@@ -96,7 +97,7 @@ def test_nonfinite_rows_stay_with_the_rows_that_see_them(gpu_lib, kind, causal, 
 def test_values_of_several_kinds_in_many_tiles(gpu_lib):
     """Infinities of both signs and NaN in several tiles, at first positions and new rows: every row against the formula."""
     n, L, W, hkv = 400, 64, 150, 64
-    case = make(KINDS[0], [n], new_len=L, hq=hkv, hkv=hkv, d=64, R=16, seed=5)
+    case = make(KINDS[0], [n, L, L, L], new_len=L, hq=hkv, hkv=hkv, d=64, R=16, seed=5)
     for at, ch, v in ((0, 1, math.inf), (200, 2, math.nan), (260, 3, -math.inf), (300, 4, math.inf), (330, 4, -math.inf),
                       (370, 5, math.inf), (399, 63, math.nan)):
         case.v_rows[0][at, 7, ch] = v
@@ -119,7 +120,7 @@ def test_values_of_several_kinds_in_many_tiles(gpu_lib):
 def test_bad_pages_and_hidden_ones(gpu_lib, kind):
     """A page id outside the pool makes the rows NaN that see one of its positions, and no others."""
     L, W = 64, 10
-    case = make(kind, [100, 164, 300, 64], new_len=L, hq=16, hkv=16, d=64, R=16, seed=3)
+    case = make(kind, [100, 164, 300, 64], new_len=L, hq=64, hkv=64, d=64, R=16, seed=3)
     c = case.to_gpu()
     hide(case, c, W, 3)
     good, gl = run_window(case, c, W, 3)
@@ -136,14 +137,14 @@ def test_bad_pages_and_hidden_ones(gpu_lib, kind):
 
 @pytest.mark.parametrize("causal", [0, 1])
 def test_more_new_rows_than_positions(gpu_lib, causal):
-    case = make(KINDS[0], [3, 0, 200, 70], new_len=70, new=[70, 70, 70, 70], hq=16, hkv=16, d=64, R=16, causal=causal, seed=4)
+    case = make(KINDS[0], [3, 0, 200, 70], new_len=70, new=[70, 70, 70, 70], hq=32, hkv=32, d=64, R=16, causal=causal, seed=4)
     o, lse = run_window(case, case.to_gpu(), 20, 1)
     check(case, o, lse, 20, 1)
     assert torch.all(o[1] == 0) and torch.all(lse[1] == -math.inf)
 
 
 def test_scores_of_minus_infinity_and_large_ones(gpu_lib):
-    case = make(KINDS[0], [300], new_len=64, hq=64, hkv=64, d=64, R=16, seed=6, sigma=3.0)
+    case = make(KINDS[0], [300], new_len=64, hq=256, hkv=256, d=64, R=16, seed=6, sigma=3.0)
     case.k_rows[0][150:280, 5, 0] = -math.inf
     case.q[:, :, 5, 0] = 1.0
     case.place()
