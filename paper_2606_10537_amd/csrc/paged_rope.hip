@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
   if (turn) {
     const double rest = (double)pair * a.step_rest * -0.6931471805599453;
     freq = exp2(-(double)pair * a.step) * (1.0 + (rest + 0.5 * rest * rest)) * 0.15915494309189535;
-    if (!a.pos) {
+    if (!a.pos && hi - lo > 256 / P) {
       const double turns = (double)(256 / P) * freq;
       sincospi(2.0 * (turns - rint(turns)), &step_sin, &step_cos);
     }

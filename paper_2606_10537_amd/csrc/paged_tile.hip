@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
   const int head = g * p.G + a.by_group.rem(rr, nr);
   const long long q_el = (((long long)b * p.Ln + nr) * p.Hq + head) * D;
   const int own = len - n_new + nr;                                // its position
-  const int lim = r >= rows ? 0 : p.causal ? own + 1 : len, low = own - a.window + 1;
+  const int lim = r >= rows ? 0 : p.causal ? own + 1 : len, low = max(own - a.window + 1, 0);
   bf16x8 qf[KS];
 #pragma unroll
   for (int i = 0; i < KS; ++i) qf[i] = *(const bf16x8*)((const uint16_t*)a.q + q_el + 16 * i + 8 * hi);

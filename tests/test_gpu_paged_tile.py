@@ -138,9 +138,10 @@ def test_bad_pages_and_hidden_ones(gpu_lib, kind):
 @pytest.mark.parametrize("causal", [0, 1])
 def test_more_new_rows_than_positions(gpu_lib, causal):
     case = make(KINDS[0], [3, 0, 200, 70], new_len=70, new=[70, 70, 70, 70], hq=32, hkv=32, d=64, R=16, causal=causal, seed=4)
-    o, lse = run_window(case, case.to_gpu(), 20, 1)
-    check(case, o, lse, 20, 1)
-    assert torch.all(o[1] == 0) and torch.all(lse[1] == -math.inf)
+    for window, sinks in ((20, 1), ((1 << 31) - 1, (1 << 31) - 1)):
+        o, lse = run_window(case, case.to_gpu(), window, sinks)
+        check(case, o, lse, window, sinks)
+        assert torch.all(o[1] == 0) and torch.all(lse[1] == -math.inf)
 
 
 def test_scores_of_minus_infinity_and_large_ones(gpu_lib):

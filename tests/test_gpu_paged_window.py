@@ -268,3 +268,23 @@ def test_long_caches(gpu_lib):
     c["cache"] = _lib.PagedCache(dims, c["k"], c["v"], table, kv, c["new_rows"])
     o, lse = run_window(case, c, W, 0, dims=dims)
     check(case, o, lse, W, 0)
+
+
+@pytest.mark.parametrize("L", [1, 40])
+def test_two_calls_at_once(gpu_lib, L):
+    """Two streams, each with a cache, outputs and a workspace of its own, over and over: the bits of a call alone."""
+    cases = [make(KINDS[i], [900 + 300 * i, 1500, 77], new_len=L, hq=16, hkv=4, d=128, R=16, seed=20 + i) for i in range(2)]
+    held = [case.to_gpu() for case in cases]
+    want = [run_window(case, c, 700, 4) for case, c in zip(cases, held)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [torch.empty(_lib.pd_paged_window_workspace_bytes(case.dims, 700, 4) + 16, dtype=torch.uint8, device="cuda") for case in cases]
+    outs = [[(torch.full_like(w[0], 7.0), torch.full_like(w[1], 7.0)) for _ in range(20)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for s in range(2):
+            with torch.cuda.stream(streams[s]):
+                o, l = outs[s][i]
+                _lib.pd_paged_window_attn(cases[s].dims, held[s]["cache"], held[s]["q"], 700, 4, o, l, workspace=ws[s])
+    torch.cuda.synchronize()
+    for s in range(2):
+        assert all(torch.equal(o, want[s][0]) and torch.equal(l, want[s][1]) for o, l in outs[s])

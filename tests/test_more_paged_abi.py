@@ -162,3 +162,29 @@ def test_binding_checks_rope_calls(lib):  # noqa: F811
                      (dict(k_new=fused[:, :, 8:12:2]), "contiguous"), (dict(w_q=torch.zeros(128, dtype=torch.bfloat16)), "GPU")):
         with pytest.raises(ValueError, match=text):
             _lib.pd_paged_append_rope(d, c, **dict(good, **kw))
+
+
+def test_rows_of_a_projection(lib):  # noqa: F811
+    """The stride that the binding finds for a strided [B, L, heads, d] is that of every row; other layouts are refused."""
+    g = torch.Generator().manual_seed(0)
+    for _ in range(300):
+        B, L, H, d, extra = (int(torch.randint(lo, hi, (), generator=g)) for lo, hi in ((1, 4), (1, 4), (1, 4), (1, 5), (0, 3)))
+        t = torch.zeros(B, L, H + extra, d)[:, :, :H]
+        ptr, stride = _lib._rows("t", t, (B, L, H, d), torch.float32, -1)
+        assert ptr == t.data_ptr()
+        for b in range(B):
+            for r in range(L):
+                assert t[b, r].data_ptr() == ptr + 4 * (b * L + r) * stride
+    base = torch.zeros(4, 6, 8, 16)
+    for bad in (base[:, ::2], base[:, :, ::2], base.transpose(1, 2), base[..., ::2], base[:, 1:4]):
+        shape = tuple(bad.shape)
+        if bad.is_contiguous():
+            continue
+        try:
+            ptr, stride = _lib._rows("t", bad, shape, torch.float32, -1)
+        except ValueError:
+            continue
+        for b in range(shape[0]):
+            for r in range(shape[1]):
+                assert bad[b, r].data_ptr() == ptr + 4 * (b * shape[1] + r) * stride
+                assert bad[b, r].is_contiguous()
