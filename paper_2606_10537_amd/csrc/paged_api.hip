@@ -234,6 +234,7 @@ pd_status launch_attn(const pd_paged_dims* d, const pd_paged_cache* cache, const
   a.part_rows = plan.part_rows;
   a.max_chunks = plan.max_chunks;
   a.per_part = 1.0f / plan.parts;
+  a.places = (float)pd::paged_places(a.c.fp4, (long long)a.c.G * a.c.Ln);
   a.grid = plan.grid;
   a.by_group = pd::fast_div(a.c.G);
   a.by_heads = pd::fast_div(a.c.Hkv);

@@ -14,8 +14,7 @@
 //   evenly; rows whose keys are cut are joined by a second kernel.
 //
 // Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
-// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; in 4 bits 209 us, 5.5 TB/s (its loads
-// alone 170, its arithmetic alone 172: conversions and the matrix products of one row in 16); 64 ragged sequences of up to
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; in 4 bits 190 us, 6.0 TB/s; 64 ragged sequences of up to
 // 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s (its loads bound it: 368 us with the arithmetic
 // of the whole steps left out, 215 with their loads left out).  One token of one 8K sequence takes 7.2 +
 // 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
@@ -59,7 +58,8 @@ struct PagedPart {
 // launch before has left, paged_plan_kernel).
 //
 // The quota: units of one size (the longest at most 5/4 of the mean), as many as the CUs or fewer,
-// or nearly twice as many, are cut into as few parts as give every CU one.  Otherwise parts of 16
+// or nearly twice as many, are cut into as few parts as give every CU one (three of 8 blocks or more in 4 bits,
+// paged_places).  Otherwise parts of 16
 // blocks or more, paged_parts of them where the keys suffice, so that the workgroups of short
 // sequences and the ends of long ones fill in.  Measured:
 // 8 x 32 heads x 8K keys 160 us, 174 in such finer parts; 16 of them 327 and 326, 15 of them 311
@@ -105,9 +105,10 @@ __device__ __forceinline__ int paged_quota(const PagedAttnArgs& a, float all, in
     const int c = (int)fminf(x, 1073741824.f);
     return (float)c < x ? c + 1 : c;
   };
-  const int fill = ceil_of(all * (1.f / kNumCu)), fine = ceil_of(all * a.per_part);
+  const float places = all >= 8.f * a.places ? a.places : 1.f * kNumCu;
+  const int fill = ceil_of(all / places), fine = ceil_of(all * a.per_part);
   const bool even = 0.8f * (float)most * seqs <= all &&
-                    (seqs <= 1.f * kNumCu || (seqs >= 1.8f * kNumCu && seqs <= 2.f * kNumCu));
+                    (seqs <= places || (seqs >= 1.8f * places && seqs <= 2.f * places));
   return max(1, uniform(even ? fill : max(fine, min(fill, 16))));
 }
 // Order: the parts of a whole quota, then the shorter ends, which even out when the

@@ -124,6 +124,7 @@ struct PagedAttnArgs {
   int row_blocks, part_rows;
   int max_chunks;        // parts of a unit at most; 1: no parts, no join
   float per_part;        // 1 / paged_parts
+  float places;          // workgroups that an even batch is cut for (paged_places)
   long long grid;
   FastDiv by_group, by_heads, by_rows, by_blocks, by_units;  // G, H_kv, G * L_n, row_blocks, H_kv * row_blocks
 };
@@ -134,6 +135,10 @@ struct PagedAttnArgs {
 // 4096), but 4 us for a thousand of those with more than 16 rows, of which it holds one
 // (8 rows of 4 heads over 8 x 8K keys 51.2 us with 1024, 54.1 with 2048, 56.5 with 2900).
 inline int paged_parts(long long rows) { return rows <= 16 ? 3328 : 1024; }
+// Workgroups that an even batch's keys are cut for where each gets 8 blocks or more: one a CU, whose waves have
+// enough loads in flight, 16 KB each, with bf16; three in 4 bits, 4 KB a wave (8 x 32 heads x 32K keys 212 us with one, 190
+// with three; 2 of them 60.8 and 54.5; 1 sequence of 4 heads, 1.3 blocks each with three, 12.9 and 14.9).
+inline int paged_places(bool fp4, long long rows) { return fp4 && rows <= 16 ? 3 * 256 : 256; }
 // Blocks up to which no unit's keys are cut, and no join follows: 16 where the units alone fill
 // the card (32 ragged sequences of 8 heads, 8 new rows, up to 600 / 2048 keys: cut 26.3 and 44.5 us,
 // whole 16.4 and 36.8; 12 of 32 heads up to 4096 keys, cut 85, whole 95), 4 elsewhere (8 heads

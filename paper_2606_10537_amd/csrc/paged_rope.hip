@@ -8,9 +8,9 @@
 // pages hold the bits of the formula whatever the order of its sums.  A double product takes 5.7 cycles of a SIMD here,
 // an fp32 one 3.8.
 //
-// Measured: prompts of 4 sequences of up to 4161 rows, 32 + 32 + 32 heads, bf16: 128 us, 4.0 TB/s; without norm and
-// rotation 98, so that the arithmetic (some 60 us of the vector units) hides behind memory only in part.  One token of
-// 8 sequences of 36 heads 9 us: a chain of lengths, page number, sine and cosine, rows.
+// Measured: prompts of 4 sequences of up to 4161 rows, 32 + 32 + 32 heads, bf16: 125 us, 4.1 TB/s; without norm and
+// rotation 91, so that the arithmetic (some 60 us of the vector units) hides behind memory only in part.  One token of
+// 8 sequences of 36 heads 8.3 us: a chain of lengths, page number, sine and cosine, rows.
 #include <type_traits>
 
 #include "paged_common.h"
@@ -35,7 +35,7 @@ __device__ __forceinline__ double flip(double x, uint32_t sign) {
 // values), so that the bounds of a page need no atomics in memory.  It walks the page's rows T at a time: sines and
 // cosines of the next T rows go to LDS in double while these are worked on, and a wave takes a head of the T rows, U loads
 // of HP rows, with the next head's in flight (172 us without, for the prompts above).  Three waves a SIMD: four spill
-// registers (174 us).
+// registers, and spilled ones are written and read through memory (174 us).
 template <int CT, int D>
 __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArgs a) {
   constexpr bool BF16 = CT != kFp32;
@@ -123,12 +123,6 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
       if (h + 4 < h1) fetch(next, r0, h + 4);
       else if (r0 + T < hi) fetch(next, r0 + T, h0 + wave);
       const void* weights = kind == 0 ? a.w_q : a.w_k;
-      float least[E], most[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        least[e] = INFINITY;
-        most[e] = -INFINITY;
-      }
       const CacheRow<CT, D> to(p, kind == 2, ((long long)page * p.Hkv + hh) * p.R, c);
       // K: the kind of head, or 3 where it is looked at here; FULL: with norm and rotation, no branch for either, so that
       // the U loads' chains run beside each other.
@@ -136,15 +130,8 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
         constexpr int K = decltype(kind_of)::value;
         constexpr bool FULL = decltype(all)::value;
         const bool norm = FULL || (kind < 2 && weights), rotates = FULL || (kind < 2 && turn);
-        double w[E];
-        if (norm) {
-          Row16<BF16> t;
-          float f[E];
-          t.load((const char*)weights + c * 16);
-          t.unpack(f);
-#pragma unroll
-          for (int e = 0; e < E; ++e) w[e] = (double)f[e];
-        }
+        Row16<BF16> weight;
+        if (norm) weight.load((const char*)weights + c * 16);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int r = r0 + u * HP + lane / L, t = min(r, hi - 1) - r0;   // rows behind the last are that one again
@@ -155,11 +142,16 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
 #pragma unroll
             for (int e = 0; e < E; ++e) z[e] = (double)y[e];
             if (norm) {
+              // Unpacked for each load: kept in double, the weights are eight registers more, and spilled ones cost writes.
+              float w[E];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) asm("" : "+v"(weight.v[i]));
+              weight.unpack(w);
               double s = 0.0;
 #pragma unroll
               for (int e = 0; e < E; ++e) {
                 s = fma(z[e], z[e], s);
-                z[e] *= w[e];
+                z[e] *= (double)w[e];
               }
               scale = inv_sqrt(lanes_sum<L>(s) * (1.0 / D) + (double)a.eps);
             }
@@ -188,12 +180,13 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
               else x[u].store(at);
             }
           } else {
-            if (K == 1 || (K == 3 && kind == 1)) {
+            if ((K == 1 || (K == 3 && kind == 1)) && p.k_bounds) {
+              // The rows that a wave holds side by side meet in LDS; NaN is neither less nor more than what is there.
+              const bool counts = FULL || r >= 0;
 #pragma unroll
               for (int e = 0; e < E; ++e) {
-                const float z = FULL || r >= 0 ? y[e] : NAN;
-                least[e] = fminf(least[e], z);
-                most[e] = fmaxf(most[e], z);
+                __hip_atomic_fetch_min(&bound[h - h0][0][e * L + c], counts ? y[e] : INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                __hip_atomic_fetch_max(&bound[h - h0][1][e * L + c], counts ? y[e] : -INFINITY, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
               }
             }
             to.put(x[u], y, r & (p.R - 1), r < hi && (FULL || r >= 0) && there);
@@ -204,13 +197,6 @@ __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArg
       if (full && kind == 0) work(std::integral_constant<int, 0>{}, std::true_type{});
       else if (full && kind == 1) work(std::integral_constant<int, 1>{}, std::true_type{});
       else work(std::integral_constant<int, 3>{}, std::false_type{});
-      if (kind == 1 && p.k_bounds) {   // the rows that a wave holds side by side meet in LDS
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          __hip_atomic_fetch_min(&bound[h - h0][0][e * L + c], least[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-          __hip_atomic_fetch_max(&bound[h - h0][1][e * L + c], most[e], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-        }
-      }
     }
   }
   if (!p.k_bounds || !there) return;
