@@ -452,8 +452,8 @@ pd_status pd_paged_read(const pd_paged_dims *dims, const pd_paged_cache *cache, 
  * of  sum_i q_i * (q_i >= 0 ? hi_i : lo_i)  with the page's bounds lo, hi: no
  * key of the page, as it was given to pd_paged_append, has a larger product with the
  * row.  The keys that an E4M3 cache holds of them are rounded, by at most 2^-4 of an
- * element, 2^-17 of the row's largest or 2^-110, so their products may exceed the
- * score by as much.  Products and sums are in double precision.  The top_k best of
+ * element, 2^-17 of the row's largest or 2^-110 (E2M1: 1/5 of an element, 1/12 of the
+ * largest of its 32 or 2^-102), so their products may exceed the score by as much.  Products and sums are in double precision.  The top_k best of
  * the sequence's ceil(kv_len/R) pages are kept; its first n_first and last n_last
  * pages rank above all others, a NaN score above every number, and ties go to the
  * lower page.
@@ -509,6 +509,8 @@ pd_status pd_paged_attn(const pd_paged_dims *dims, const pd_paged_cache *cache, 
  * pages: o, lse, rows that see nothing, page ids outside the pool, values that are
  * not finite, rounding.
  * Sizes: window >= 1, n_sinks >= 0 (those beyond all positions count as all).
+ * Which kernel runs, and whether long windows are cut over workgroups, goes by the sizes
+ * in dims: give L_n the most new rows of the call, not more.
  * workspace: >= pd_paged_window_workspace_bytes(dims, window, n_sinks) bytes (may be
  * 0, then workspace may be NULL), which grow with the window and not with max_pages.
  */

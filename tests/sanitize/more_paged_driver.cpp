@@ -66,8 +66,10 @@ int main() {
   huge.batch = 65536; huge.n_heads_q = 16384; huge.n_heads_kv = 16384; huge.new_len = 2; huge.max_pages = 1 << 24;
   EXPECT(window(huge, INT32_MAX, INT32_MAX, big), PD_ERR_BAD_DIMS);
   EXPECT(rope(huge, 1 << 21, 1 << 21, 1 << 21, 1e-6f, 1e4, A), PD_ERR_BAD_DIMS);
-  huge.batch = 1; huge.n_heads_q = huge.n_heads_kv = 1; huge.new_len = 1 << 24; huge.causal = 0;
+  huge.batch = 1; huge.n_heads_q = huge.n_heads_kv = 1; huge.new_len = 1 << 13; huge.causal = 0;
   if (pd_paged_window_workspace_bytes(&huge, INT32_MAX, INT32_MAX) == 0) { std::printf("FAIL: no size for many new rows\n"); ++failures; }
+  huge.new_len = 1 << 24;   // row blocks that fill the card: nothing is cut
+  EXPECT(pd_paged_window_workspace_bytes(&huge, INT32_MAX, INT32_MAX), 0);
   for (int64_t s : {INT64_MIN, int64_t(0), INT64_MAX}) {
     EXPECT(rope(d, s, 256, 256, 1e-6f, 1e4, A), PD_ERR_BAD_DIMS);
     EXPECT(rope(d, 1024, s, 256, 1e-6f, 1e4, A), PD_ERR_BAD_DIMS);

@@ -46,3 +46,14 @@ def test_packing(d):
     assert byte.dtype is torch.uint8 and byte.shape == (5, d // 2)
     assert int(byte[0, 0]) == codes[0, 0] | codes[0, 1] << 4
     assert np.array_equal(unpack4(byte.numpy()), codes)
+
+
+def test_how_far_a_held_element_is_off():
+    """At most 1/5 of itself, 1/12 of the largest of its 32, or 2^-102 (a quarter of the least power of two)."""
+    rng = np.random.default_rng(2)
+    x = rng.standard_normal((200, 64)) * 2.0 ** rng.integers(-130, 120, (200, 1))
+    x[:40] = np.linspace(-6, 6, 40 * 64).reshape(40, 64)
+    x[:, 0] = np.abs(x).max(-1)
+    off = np.abs(ref.held4_ref(*ref.quantise4_ref(x)) - x)
+    most = np.repeat(np.abs(x.reshape(200, 2, 32)).max(-1), 32, -1)
+    assert np.all(off <= np.maximum(np.maximum(np.abs(x) / 5, most / 12), 2.0 ** -102) * (1 + 2.0 ** -50))
