@@ -1,8 +1,8 @@
 // Attention of many new rows over the pages, within a sliding window: chunks of a prompt.
 //
 // The kernel of paged_attn.hip takes 32 query rows a workgroup, so that every key of a window is read and converted for
-// 32 rows, and its 16-row products leave half of the matrix cores' rate.  Here a workgroup of four waves takes 64 or 128 rows
-// of a KV head; the keys go through LDS in tiles of 64, as bf16 whatever the pages hold, and a wave multiplies 32 rows with
+// 32 rows, and its 16-row products leave half of the matrix cores' rate.  Here a workgroup takes 64 or 128 rows of
+// a KV head; the keys go through LDS in tiles of 128 or 64, as bf16 whatever the pages hold, and a wave multiplies 32 rows with
 // v_mfma_f32_32x32x16_bf16.  The next tile is on its way in registers while one is multiplied; one barrier a tile.
 //
 //   S^T = K Q^T: row = key, column = query row; element e of a lane is key 8 (e / 4) + 4 (lane / 32) + e % 4 of 32.
@@ -10,8 +10,8 @@
 //     keys of a channel, comes from the rows of V by ds_read_b64_tr_b16 (among 16 lanes, lane j receives element j % 4 of
 //     what lanes j / 4, 4 + j / 4, .. point at).
 //
-// ROWS: 128 rows, 32 a wave; 64, with two waves on the same 32 rows and half of each tile's keys, joined at the end,
-// where there are few row blocks.
+// ROWS: 128 rows, four waves of 32; 64, with four of eight waves on the same 32 rows and a quarter of each tile's keys
+// each, joined at the end, where there are few row blocks.
 #include "paged_common.h"
 
 namespace pd {
@@ -200,6 +200,19 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
 #pragma unroll
       for (int i = 0; i < KS; ++i)
         s = mfma32x32x16(*(const bf16x8*)&kt[tile_at<KEYS>(32 * blk + n, 2 * i + hi)], qf[i], s);
+      // The block's V, on its way during the softmax.  512 rows of 8 x 4 heads behind 7.5K keys, a window of 1024: 28.5 us
+      // with V read at its products, 27.1 so; with a window of 4096, 72 and 67.  At 128 rows a workgroup both are alike.
+      i16x8 v[DB][2];
+#pragma unroll
+      for (int i = 0; i < DB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PD_LDS i16x4*)(vt + v_at[x] + i * (KEYS * 32) + (32 * blk + 16 * h) * 32));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][h][4 * x + j] = z[j];
+          }
       // The block's two groups: their positions, and whether all rows see them.
       int pos[2];
       bool bad[2], whole = true;
@@ -259,16 +272,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
 #pragma unroll
       for (int i = 0; i < DB; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          i16x8 v;
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const i16x4 z = __builtin_amdgcn_ds_read_tr16_b64_v4i16((PD_LDS i16x4*)(vt + v_at[x] + i * (KEYS * 32) + (32 * blk + 16 * h) * 32));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * x + j] = z[j];
-          }
-          o[i] = mfma32x32x16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w[h]), o[i]);
-        }
+        for (int h = 0; h < 2; ++h)
+          o[i] = mfma32x32x16(__builtin_bit_cast(bf16x8, v[i][h]), __builtin_bit_cast(bf16x8, w[h]), o[i]);
       if (odd_tile[t & 3]) {
         // Values that are not finite, from the pages, to the rows that see their key: with its weight, so that where this
         // has underflowed an infinity gives NaN.
