@@ -204,7 +204,7 @@ Window window_of(const pd_paged_dims* d, int window, int n_sinks) {
   w.most_keys = w.keys + (d->causal ? 0 : (long long)d->new_len);
   // The tile kernel scales scores that it has masked with -inf: not where the scale may vanish in fp32.
   if (!(d->sm_scale > 0.f) || d->sm_scale >= 1e-30f)
-    w.tile_rows = pd::paged_tile_rows(d->dtype == PD_BF16, (long long)d->batch * d->n_heads_kv, (long long)G * d->new_len);
+    w.tile_rows = pd::paged_tile_rows(d->dtype == PD_BF16, (long long)d->batch * d->n_heads_kv, (long long)G * d->new_len, w.most_keys);
   return w;
 }
 

@@ -151,15 +151,19 @@ constexpr int kPlanBatch = 128;
 // Keys that one workgroup takes at a time.
 int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
-// Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does, which cuts
-// the keys of few row blocks (8 heads x 4 query heads, window 1024, 256 new rows: 128 blocks of 64 rows 25.7 us, 19.5 there;
-// 512 new rows: 256 blocks 28.4, 35.4 there; window 8192, 64 new rows: 128 and 35).  128 rows where these fill the card and
-// few of them are empty (2 sequences of 512 new rows 44.5 us, 50.5 with 64; 8 of them 124 and 203; 64 of 16 new rows, 64 a
-// head: 76.6 and 70.7).
-inline int paged_tile_rows(bool bf16, long long pairs, long long rows) {
-  const long long small = pairs * ((rows + 63) / 64), large = pairs * ((rows + 127) / 128);
-  if (!bf16 || rows < 64 || small < 256) return 0;
-  return large >= 256 && 2 * small > 3 * large ? 128 : 64;
+// Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does, whose blocks
+// of 32 rows take a CU each, with the keys cut where there are fewer of them (8 heads x 4 query heads, window 1024: 256
+// new rows, 256 blocks of 32, 19.9 us and 24 as 128 blocks of 64; 272 new rows 34 and 24.5; window 4096, 240 new rows 62 and
+// 66, 272 83 and 66; 24 sequences of 9 new rows 36 and 29.5).  128 rows where they take fewer rounds of the card (2
+// sequences of 512 new rows 42 us, 48.6 with 64; 8 of them 109 and 186; 12 of 80 new rows, two rounds either way, 60 and
+// 51).  Over few keys (`keys`: of 32 rows) also where they take as many but more than one, as two workgroups a CU then
+// hide each other's start (64 sequences of 16 new rows, window 256: 25.4 and 31.2; window 1024 67 and 69; 128
+// sequences of 9 new rows, window 4000: 438 and 368).
+inline int paged_tile_rows(bool bf16, long long pairs, long long rows, long long keys) {
+  const long long blocks = pairs * ((rows + 31) / 32), small = pairs * ((rows + 63) / 64), large = pairs * ((rows + 127) / 128);
+  if (!bf16 || rows <= 32 || blocks <= 256) return 0;
+  const long long rounds = (small + 255) / 256, large_rounds = (large + 255) / 256;
+  return large_rounds < rounds || (large_rounds == rounds && rounds > 1 && keys <= 512) ? 128 : 64;
 }
 hipError_t launch_paged_tile(PagedAttnArgs a, int rows, hipStream_t s);
 

@@ -41,6 +41,17 @@ def test_128_rows_a_workgroup(gpu_lib, kind):
             run("128", kind, lens, 90, 4, new_len=L, new=new, hq=64, hkv=16, d=d, R=16, causal=causal, seed=d)
 
 
+@pytest.mark.parametrize("kind", KINDS, ids=IDS)
+@pytest.mark.parametrize("B,L,hq,hkv,d,R", [(5, 33, 28, 28, 64, 16), (3, 9, 180, 45, 128, 16), (1, 260, 32, 8, 128, 64), (1, 449, 16, 4, 64, 128),
+                                            (4, 48, 136, 136, 64, 32)])
+def test_blocks_around_the_least_that_fill_the_card(gpu_lib, kind, B, L, hq, hkv, d, R):
+    """Blocks of 32 rows just above 256, and below: fewer than 64 rows a KV head, many."""
+    lens = [900, 5, L + 13, 0, 333][:B]
+    for causal in (0, 1):
+        for window in (70, 600):
+            run("around", kind, lens, window, 3, new_len=L, new=[L, min(5, L), L - 1, 0, L][:B], hq=hq, hkv=hkv, d=d, R=R, causal=causal, seed=L)
+
+
 def test_more_than_sixteen_tiles(gpu_lib):
     """Windows of more than 1024 positions: where their groups lie is looked up again."""
     for window, sinks in ((2500, 130), (1 << 30, 0)):
@@ -63,7 +74,18 @@ def test_the_same_bits_again_and_no_workspace(gpu_lib):
 def test_nonfinite_rows_stay_with_the_rows_that_see_them(gpu_lib, kind, causal, which, d):
     """A NaN or an infinity at a position: the rows that do not see it keep their bits; the others get what the formula
     gives, also where all rows of a tile see it."""
-    L, W, n, hkv = 70, 30, 200, 128
+    check_nonfinite(kind, causal, which, d, 70, 128)
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=IDS)
+@pytest.mark.parametrize("L,hkv", [(40, 136), (70, 256)])
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_nonfinite_rows_in_blocks_of_64_and_of_128(gpu_lib, kind, which, L, hkv):
+    check_nonfinite(kind, 1, which, 64, L, hkv)
+
+
+def check_nonfinite(kind, causal, which, d, L, hkv):
+    W, n = 30, 200
     for bad in ((math.nan,) if kind[1] != PD_BF16 else (math.nan, math.inf, -math.inf)):
         for at in (1, 120, 150, 199):
             case = make(kind, [n], new_len=L, hq=hkv, hkv=hkv, d=d, R=16, causal=causal, seed=12)
