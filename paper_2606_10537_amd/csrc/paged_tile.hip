@@ -12,6 +12,8 @@
 //
 // ROWS: 128 rows, four waves of 32; 64, with four of eight waves on the same 32 rows and a quarter of each tile's keys
 // each, joined at the end, where there are few row blocks.
+#include <algorithm>
+
 #include "paged_common.h"
 
 namespace pd {
@@ -70,7 +72,7 @@ struct Raw8 {
 __device__ __forceinline__ uint32_t not_finite(uint32_t x) { return (x & 0x7f807f80u) + 0x00800080u; }
 
 template <int D, int CT, int ROWS, int KEYS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs a, FastDiv by_run) {
   constexpr int CH = D / 8, RP = 64 * WAVES / CH, NP = KEYS / RP;   // chunks of a row, rows of a load, loads of a tile
   constexpr int KP = 32 * WAVES / ROWS;                            // waves that share their rows
   constexpr int NB = KEYS / 32 / KP;                               // blocks of 32 keys of a wave in a tile
@@ -80,8 +82,11 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
   __shared__ __attribute__((aligned(16))) uint16_t lds[2][2][TILE];   // [buffer][K, V]
   __shared__ int odd_tile[4];                                      // a value of tile t is not finite: word t % 4
   const PagedArgs& p = a.c;
-  if (block_id() >= (uint32_t)a.grid) return;
-  const int id = xcd_remap(uniform((int)block_id()), (int)a.grid);   // row blocks of the same keys on one XCD
+  // Workgroup i runs on XCD i % 8: runs of row blocks, which read the same keys, go to the XCDs in turn.
+  const uint32_t i = uniform((int)block_id());
+  const int turn = by_run.quot(i / kNumXcd);
+  const int id = (turn * kNumXcd + i % kNumXcd) * by_run.d + by_run.rem(i / kNumXcd, turn);
+  if (id >= (int)a.grid) return;
   const int bg = a.by_blocks.quot(id), rb = a.by_blocks.rem(id, bg);
   const int b = a.by_heads.quot(bg), g = a.by_heads.rem(bg, b);
   const int wave = uniform((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63, n = lane & 31, hi = lane >> 5;
@@ -89,12 +94,12 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
   if (row0 >= rows) return;
   const int first_row = row0 + wave / KP * 32;                     // of the wave; beyond `rows`: none of them is real
 
-  // This lane's query row.
+  // This lane's query row; lanes beyond the last repeat it, so that a block of few rows needs no masks for them.
   const int r = first_row + n, rr = min(r, rows - 1), nr = a.by_group.quot(rr);
   const int head = g * p.G + a.by_group.rem(rr, nr);
   const long long q_el = (((long long)b * p.Ln + nr) * p.Hq + head) * D;
   const int own = len - n_new + nr;                                // its position
-  const int lim = r >= rows ? 0 : p.causal ? own + 1 : len, low = max(own - a.window + 1, 0);
+  const int lim = p.causal ? own + 1 : len, low = max(own - a.window + 1, 0);
   bf16x8 qf[KS];
 #pragma unroll
   for (int i = 0; i < KS; ++i) qf[i] = *(const bf16x8*)((const uint16_t*)a.q + q_el + 16 * i + 8 * hi);
@@ -106,7 +111,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
   const int far = (min(a.n_sinks, end) + 15) / 16, from = max(max(any_low, 0) / 16, far);
   const int groups = far + max(0, (end + 15) / 16 - from), tiles = (groups + GT - 1) / GT;
   // Those that all rows of the wave, and of the workgroup, see.
-  const int every = first_row + 31 >= rows ? 0 : p.causal ? position(first_row) + 1 : len;
+  const int every = p.causal ? position(first_row) + 1 : len;
   const int all_low = position(first_row + 31) - a.window + 1;
   const int wg_every = p.causal ? position(row0) + 1 : len, wg_low = position(row0 + ROWS - 1) - a.window + 1;
 
@@ -325,7 +330,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
       const bool more = t + 1 < tiles;
       tile = tile + 1 < tiles ? tile + 1 : 0;
       if (more) fetch(tile);
-      multiply(here, t, pages, positions);
+      if (first_row < rows) multiply(here, t, pages, positions);
       if (more) put(t + 1);
       __syncthreads();
       // Every wave has read the word; it is set for tile t + 4 three barriers on.
@@ -393,8 +398,15 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
 
 template <int D, int CT>
 hipError_t paged_tile_of(const PagedAttnArgs& a, int rows, hipStream_t s) {
-  if (rows == 128) hipLaunchKernelGGL((paged_tile_kernel<D, CT, 128, 64, 4>), grid_xy(a.grid), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged_tile_kernel<D, CT, 64, 128, 8>), grid_xy(a.grid), dim3(512), 0, s, a);
+  // The longest runs that deal every sequence to all XCDs: where few sequences of a batch have many new rows, one
+  // range of ids an XCD leaves them to a part of the card.
+  int heads = 1;
+  while (heads < kNumXcd && a.c.Hkv % (2 * heads) == 0) heads *= 2;
+  const int run = std::min(((int)a.row_blocks * heads + kNumXcd - 1) / kNumXcd, 256);
+  const long long runs = (a.grid + run - 1) / run, grid = (runs + kNumXcd - 1) / kNumXcd * kNumXcd * run;
+  const FastDiv by_run = fast_div(run);
+  if (rows == 128) hipLaunchKernelGGL((paged_tile_kernel<D, CT, 128, 64, 4>), grid_xy(grid), dim3(256), 0, s, a, by_run);
+  else hipLaunchKernelGGL((paged_tile_kernel<D, CT, 64, 128, 8>), grid_xy(grid), dim3(512), 0, s, a, by_run);
   return hipGetLastError();
 }
 
