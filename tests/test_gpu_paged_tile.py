@@ -47,9 +47,17 @@ def test_128_rows_a_workgroup(gpu_lib, kind):
 def test_blocks_around_the_least_that_fill_the_card(gpu_lib, kind, B, L, hq, hkv, d, R):
     """Blocks of 32 rows just above 256, and below: fewer than 64 rows a KV head, many."""
     lens = [900, 5, L + 13, 0, 333][:B]
-    for causal in (0, 1):
-        for window in (70, 600):
-            run("around", kind, lens, window, 3, new_len=L, new=[L, min(5, L), L - 1, 0, L][:B], hq=hq, hkv=hkv, d=d, R=R, causal=causal, seed=L)
+    for causal, window in ((1, 70), (0, 600)):
+        run("around", kind, lens, window, 3, new_len=L, new=[L, min(5, L), L - 1, 0, L][:B], hq=hq, hkv=hkv, d=d, R=R, causal=causal, seed=L)
+
+
+@pytest.mark.parametrize("hq,hkv,L", [(24, 24, 257), (12, 12, 530), (32, 8, 128), (39, 13, 100), (4, 2, 520)])
+def test_padded_batches(gpu_lib, hq, hkv, L):
+    """Most sequences with one new row or none: the row blocks that hold rows lie far apart, in runs of odd and even length."""
+    B = 16
+    new = [(L, 1, 1, 0, 2, 1, 70, 1)[i % 8] for i in range(B)]
+    lens = [n + (0, 40, 211, 7, 500)[i % 5] for i, n in enumerate(new)]
+    run("padded", KINDS[L % 3], lens, 90, 3, new_len=L, new=new, hq=hq, hkv=hkv, d=64, R=16, causal=L % 2, seed=L)
 
 
 def test_more_than_sixteen_tiles(gpu_lib):
