@@ -153,17 +153,16 @@ int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
 // Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does, whose blocks
 // of 32 rows take a CU each, with the keys cut where there are fewer of them (8 heads x 4 query heads, window 1024: 256
-// new rows, 256 blocks of 32, 19.9 us and 24 as 128 blocks of 64; 272 new rows 34 and 24.5; window 4096, 240 new rows 62 and
-// 66, 272 83 and 66; 24 sequences of 9 new rows 36 and 29.5).  128 rows where they take fewer rounds of the card (2
-// sequences of 512 new rows 42 us, 48.6 with 64; 8 of them 109 and 186; 12 of 80 new rows, two rounds either way, 60 and
-// 51).  Over few keys (`keys`: of 32 rows) also where they take as many but more than one, as two workgroups a CU then
-// hide each other's start (64 sequences of 16 new rows, window 256: 25.4 and 31.2; window 1024 67 and 69; 128
-// sequences of 9 new rows, window 4000: 438 and 368).
+// new rows, 256 blocks of 32, 19 us and 24 as 128 blocks of 64; 272 new rows 34 and 24.4; window 4096, 240 new rows 62 and
+// 64, 272 83 and 65; 24 sequences of 9 new rows 37 and 28).  128 rows where they take fewer rounds of the card (2
+// sequences of 512 new rows 43 us, 49 with 64; 8 of them 110 and 184; 12 of 80 new rows, two rounds either way, 53 and
+// 50).  Also for up to 64 rows over more than one round, unless the keys are many: the waves without rows rest, and two
+// workgroups a CU hide each other's start (64 sequences of 16 new rows, windows of 256 / 1024: 22.7 / 62 and 31.3 / 70;
+// 128 sequences of 9 new rows, window 4000, in 8 bits: 335 and 315).  `keys`: that 32 rows visit at most.
 inline int paged_tile_rows(bool bf16, long long pairs, long long rows, long long keys) {
   const long long blocks = pairs * ((rows + 31) / 32), small = pairs * ((rows + 63) / 64), large = pairs * ((rows + 127) / 128);
   if (!bf16 || rows <= 32 || blocks <= 256) return 0;
-  const long long rounds = (small + 255) / 256, large_rounds = (large + 255) / 256;
-  return large_rounds < rounds || (large_rounds == rounds && rounds > 1 && keys <= 512) ? 128 : 64;
+  return (large + 255) / 256 < (small + 255) / 256 || (rows <= 64 && small > 256 && keys <= 2048) ? 128 : 64;
 }
 hipError_t launch_paged_tile(PagedAttnArgs a, int rows, hipStream_t s);
 
