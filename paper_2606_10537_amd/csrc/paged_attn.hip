@@ -769,8 +769,10 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
         }
       top = fmaxf(m[t], group_max(top));
       // The sums are brought to a new maximum only where it has risen by more than 8
-      // (a factor of 256, far from overflow).
-      if (__any(top > m[t] + 8.f)) {
+      // (a factor of 256, far from overflow), each row by itself: what a row sees does not change the rounding of others.
+      const bool up = top > m[t] + 8.f;
+      if (__any(up)) {
+        top = up ? top : m[t];
         const float f = fast_exp2(m[t] - top);
         l[t] *= f;
 #pragma unroll
