@@ -670,20 +670,24 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
     // copy of the step's values in the wave's part of lds_o.
     bool any_odd = false;
     if (CT == kFp4 && !whole && (WIN || p.causal) && n_new > 1) {
-      // A key's group of channels is NaN or holds no such value: the copy has a word for each.
+      // A key's group of channels is NaN, or some of its values read as infinity (4 and 6 times 2^126): the copy has four
+      // bits for each channel, 1 for NaN and 6 and 14 for the infinities.
       bool odd = false;
 #pragma unroll
-      for (int j = 0; j < VR; ++j) odd = odd || !(vs[j] < INFINITY);
+      for (int j = 0; j < VR; ++j) odd = odd || !(vs[j] < 0x1p126f);
       any_odd = __any(odd);
       if (any_odd) {
-        uint32_t* copy = (uint32_t*)&lds_o[wave][0][0];   // [key of the step][quarter of the channels]
+        uint32_t* copy = (uint32_t*)&lds_o[wave][0][0];   // [key of the step][lane of 16]
 #pragma unroll
         for (int j = 0; j < VR; ++j) {
+          const int at = D == 64 ? 16 * (j & 1) : 0;      // where the key's codes begin
+          uint32_t& word = y[D == 64 ? j & ~1 : j];
+          const uint32_t code = D == 64 ? word >> at & 0xffffu : word;
           const bool nan = !(vs[j] < INFINITY);
-          copy[(16 * (j / 4) + 4 * g4 + j % 4) * 4 + (n & 3)] = nan ? kNanWord : 0u;
+          const uint32_t large = vs[j] < 0x1p126f ? 0u : (code >> 1 & code >> 2 & 0x11111111u) * 15u;
+          copy[(16 * (j / 4) + 4 * g4 + j % 4) * 16 + n] = nan ? 0x11111111u : large & ((code & 0x88888888u) | 0x66666666u);
+          word &= ~((nan ? D == 64 ? 0xffffu : 0xffffffffu : large) << at);
           vs[j] = nan ? 1.f : vs[j];
-          if constexpr (D == 128) y[j] = nan ? 0u : y[j];
-          else y[j & ~1] = nan ? y[j & ~1] & (j & 1 ? 0xffffu : 0xffff0000u) : y[j & ~1];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
@@ -841,19 +845,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           o[t][i] = mfma16x16x32(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, pw), o[t][i]);
         }
       }
-      if (CT == kFp4 && !whole && any_odd) {
-#pragma unroll 1
-        for (int key = 0; key < S::KS; ++key) {
-          if (!sees(t, (key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16)) continue;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float x = __uint_as_float(((const uint32_t*)&lds_o[wave][0][0])[key * 4 + r]);   // row 4 g + r is in quarter r
-#pragma unroll
-            for (int i = 0; i < NT; ++i) o[t][i][r] += x;
-          }
-        }
-      }
-      if (CT != kFp4 && !whole && any_odd) {
+      if (!whole && any_odd) {
         for (int key = 0; key < S::KS; ++key) {
           // The row's weight of the key, from the lane that holds it: a value counts with its weight
           // as in a product, so where this has underflowed an infinity gives NaN here too.
@@ -862,15 +854,20 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
           for (int i = 1; i < 4 * H; ++i) w = (key >> 4) * 4 + key % 4 == i ? pr[i / 4][i % 4] : w;
           w = __shfl(w, 16 * (key / 4 % 4) + n);
           if (!sees(t, (key < 16 ? s.pos[0] : s.pos[H - 1]) + key % 16)) continue;
-          const uint32_t* copy = (const uint32_t*)&lds_o[wave][0][0] + key * (CT == kFp32 ? D : D / 2);
+          const uint32_t* copy = (const uint32_t*)&lds_o[wave][0][0] + key * (CT == kFp32 ? D : CT == kFp4 ? 16 : D / 2);
 #pragma unroll
           for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-              const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : S::base(4 * g4 + r) + i;
-              const uint32_t u = copy[CT == kFp32 ? ch : ch / 2];
-              const float x = __uint_as_float(CT == kFp32 ? u : i & 1 ? u & 0xffff0000u : u << 16);
-              if (!(fabsf(x) < INFINITY)) o[t][i][r] += w * x;
+              if constexpr (CT == kFp4) {
+                const uint32_t kind = copy[4 * g4 + r] >> (4 * i) & 15;   // lane m has the channels of row m
+                if (kind) o[t][i][r] += w * (kind == 1 ? NAN : kind & 8 ? -INFINITY : INFINITY);
+              } else {
+                const int ch = CT == kFp32 ? 64 * (i / 4) + 4 * (4 * g4 + r) + i % 4 : S::base(4 * g4 + r) + i;
+                const uint32_t u = copy[CT == kFp32 ? ch : ch / 2];
+                const float x = __uint_as_float(CT == kFp32 ? u : i & 1 ? u & 0xffff0000u : u << 16);
+                if (!(fabsf(x) < INFINITY)) o[t][i][r] += w * x;
+              }
             }
         }
       }
