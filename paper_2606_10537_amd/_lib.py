@@ -344,20 +344,24 @@ def _rows(name, t, shape, type_, device):
     if t.dtype is not type_ or t.shape != shape or t.get_device() != device:
         _refuse(name, t, shape, type_, device)
     heads, d = shape[-2], shape[-1]
-    if t.is_contiguous():
+    # The questions in the order of what is usual: [T, heads, d] contiguous or in rows one stride apart, [B, L, heads, d] in
+    # such rows, as those of a fused projection are.
+    dims = len(shape)
+    if dims != 4 and t.is_contiguous():
         return t.data_ptr(), heads * d
-    # [T, heads, d] and [B, L, heads, d] in rows one stride apart, as those of a fused projection are: told in a few
-    # comparisons (dimensions of one element have no stride that counts, and tensors of one row are contiguous).
     strides = t.stride()
     if strides[-1] == 1 and strides[-2] == d:
-        if len(strides) == 3:
+        if dims == 3:                      # of more than one row, as it is not contiguous
             return t.data_ptr(), strides[0]
-        if len(strides) == 4:
+        if dims == 4:
             B, L = shape[0], shape[1]
-            if L == 1:
+            if L > 1:
+                if B == 1 or strides[0] == L * strides[1]:
+                    return t.data_ptr(), strides[1]
+            elif B > 1:
                 return t.data_ptr(), strides[0]
-            if B == 1 or strides[0] == L * strides[1]:
-                return t.data_ptr(), strides[1]
+    if dims == 4 and t.is_contiguous():
+        return t.data_ptr(), heads * d
     if (d > 1 and strides[-1] != 1) or (heads > 1 and strides[-2] != d):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
     lead = [(n, s) for n, s in zip(shape[:-2], strides[:-2]) if n != 1]

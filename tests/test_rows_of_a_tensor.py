@@ -17,7 +17,7 @@ class NoStride(torch.Tensor):
         raise AssertionError("a contiguous tensor's strides were asked for")
 
 
-@pytest.mark.parametrize("shape", [(1, 3, 4), (5, 1, 4), (5, 3, 4), (2, 1, 3, 4), (1, 5, 3, 4), (2, 5, 1, 4)])
+@pytest.mark.parametrize("shape", [(1, 3, 4), (5, 1, 4), (5, 3, 4), (3, 4)])
 def test_contiguous_rows_are_told_first(shape):
     t = torch.zeros(shape).as_subclass(NoStride)
     assert rows(t) == (t.data_ptr(), shape[-2] * shape[-1])
