@@ -510,7 +510,10 @@ pd_status pd_paged_attn(const pd_paged_dims *dims, const pd_paged_cache *cache, 
  * not finite, rounding.
  * Sizes: window >= 1, n_sinks >= 0 (those beyond all positions count as all).
  * Which kernel runs, and whether long windows are cut over workgroups, goes by the sizes
- * in dims: give L_n the most new rows of the call, not more.
+ * in dims: give L_n the most new rows of the call, not more.  Where few sequences of a batch have
+ * many new rows and the others one or a few, and the window is long, two calls, one for either
+ * kind, take less than one (H_q = 32, H_kv = 8, window 8192, one sequence of 512 new rows and three of one: 314 us
+ * in one call, 119 and 24 in two).
  * workspace: >= pd_paged_window_workspace_bytes(dims, window, n_sinks) bytes (may be
  * 0, then workspace may be NULL), which grow with the window and not with max_pages.
  */

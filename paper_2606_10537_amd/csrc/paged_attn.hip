@@ -14,7 +14,7 @@
 //   evenly; rows whose keys are cut are joined by a second kernel.
 //
 // Measured: 8 x 32 heads x 32K keys 622 us, 6.9 TB/s of keys and values (a kernel that does
-// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; in 4 bits 190 us, 6.0 TB/s; 64 ragged sequences of up to
+// nothing but read reaches 6.5 to 7.1 here); in 8 bits 325 us, 6.7 TB/s; in 4 bits 186 us, 6.1 TB/s; 64 ragged sequences of up to
 // 32K, 8 heads, 8 bits, pages of 16 rows 365 us, 6.0 TB/s (its loads bound it: 368 us with the arithmetic
 // of the whole steps left out, 215 with their loads left out).  One token of one 8K sequence takes 7.2 +
 // 3.3 us, a chain of loads (arguments, lengths, page numbers, keys) in each workgroup, of which
@@ -520,7 +520,8 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
       const char* vp = (const char*)p.v_pages + row * RB + g4 * (4 * RB);
       if constexpr (CT == kFp4) {
         // The 16 rows in a line: lane n has a quarter (n % 4) of row 4 g + n / 4, and four lanes swap later.  Loads of
-        // 4 bytes, a row each, were four times as many (8 x 32 heads x 32K keys 277 us, now 230).
+        // 4 bytes, a row each, were four times as many (8 x 32 heads x 32K keys 277 and 230 us, both with weights of two
+        // terms and one part a CU).
         const char* at = (const char*)p.v_pages + row * RB;
         if constexpr (D == 128) {
           const u32x4 w = fetch<STREAM>((const u32x4*)(at + 16u * (uint32_t)lane));
@@ -820,7 +821,7 @@ __global__ __launch_bounds__(256, D == 64 && CT != kFp32 ? 3 : D == 64 || (RT ==
         // 615.1 us, one token of 8K keys 10.2 and 10.3).  Two tiles: one term, rounded to nearest; the second would be
         // paid for (32 rows of 4 heads over 8 x 8K keys 85.4 us with one, 89.1 with two; in 8 bits 84.4 and 97.9, d = 64
         // 50.3 and 57.4).  E2M1 values, whose own rounding is 2^-3 and more, take one term: their products do not hide
-        // behind the memory (8 x 32 heads x 32K keys 210 us with one term, 232 with two; 64 ragged requests 201 and 221).
+        // behind the memory (8 x 32 heads x 32K keys 183 us with one term, 203 with two; 64 ragged requests 198 and 215).
         u32x4 pw, pl;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {

@@ -153,12 +153,17 @@ int paged_block_keys(bool fp32);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
 // Query rows of a workgroup of the tile kernel, which takes windows of many rows; 0: the other kernel does, whose blocks
 // of 32 rows take a CU each, with the keys cut where there are fewer of them (8 heads x 4 query heads, window 1024: 256
-// new rows, 256 blocks of 32, 19 us and 24 as 128 blocks of 64; 272 new rows 34 and 24.4; window 4096, 240 new rows 62 and
-// 64, 272 83 and 65; 24 sequences of 9 new rows 37 and 28).  128 rows where they take fewer rounds of the card (2
-// sequences of 512 new rows 43 us, 49 with 64; 8 of them 110 and 184; 12 of 80 new rows, two rounds either way, 53 and
+// new rows, 256 blocks of 32, 18 us and 24 as 128 blocks of 64; 272 new rows 33 and 24; window 4096, 240 new rows 61 and
+// 64, 272 82 and 64; 24 sequences of 9 new rows 36 and 27).  128 rows where they take fewer rounds of the card (2
+// sequences of 512 new rows 41 us, 47 with 64; 8 of them 107 and 183; 12 of 80 new rows, two rounds either way, 53 and
 // 50).  Also for up to 64 rows over more than one round, unless the keys are many: the waves without rows rest, and two
-// workgroups a CU hide each other's start (64 sequences of 16 new rows, windows of 256 / 1024: 22.7 / 62 and 31.3 / 70;
-// 128 sequences of 9 new rows, window 4000, in 8 bits: 335 and 315).  `keys`: that 32 rows visit at most.
+// workgroups a CU hide each other's start (64 sequences of 16 new rows, windows of 256 / 1024: 22 / 62 and 31 / 70;
+// 128 sequences of 9 new rows, window 4000, in 8 bits: 334 and 315).  `keys`: that 32 rows visit at most.
+// It goes by the places of the call, as how many hold rows is known on the device alone.  Where few do, every sequence of
+// few rows still walks its window in one workgroup a head, and the other kernel, which cuts the keys, may take less (8 x 4
+// heads, window 8192, this and the other: one sequence of 512 new rows and three of one 314 us and 263, two of one row in
+// 512 places 228 and 88, eight 246 and 163; but 32 such 311 and 562, 64 in 16 places, four of them full, 358 and 431; with
+// windows of 1024 the first is 48 and 51).
 inline int paged_tile_rows(bool bf16, long long pairs, long long rows, long long keys) {
   const long long blocks = pairs * ((rows + 31) / 32), small = pairs * ((rows + 63) / 64), large = pairs * ((rows + 127) / 128);
   if (!bf16 || rows <= 32 || blocks <= 256) return 0;

@@ -5,12 +5,11 @@
 // nothing else is moved, so memory bounds it.
 //
 // Norm and rotation are in double precision: what is held in a few bits is next to a border now and then, and so the
-// pages hold the bits of the formula whatever the order of its sums.  A double product takes 5.7 cycles of a SIMD here,
-// an fp32 one 3.8.
+// pages hold the bits of the formula whatever the order of its sums.
 //
-// Measured: prompts of 4 sequences of up to 4161 rows, 32 + 32 + 32 heads, bf16: 125 us, 4.1 TB/s; without norm and
-// rotation 91, so that the arithmetic (some 60 us of the vector units) hides behind memory only in part.  One token of
-// 8 sequences of 36 heads 8.3 us: a chain of lengths, page number, sine and cosine, rows.
+// Measured: prompts of 4 sequences of up to 4161 rows, 32 + 32 + 32 heads, bf16: 121 us, 4.2 TB/s; without norm and
+// rotation 91, so that the arithmetic (counters: 60 us of the vector units) hides behind memory only in part.  One token
+// of 8 sequences of 36 heads 8.4 us: a chain of lengths, page number, sine and cosine, rows.
 #include <type_traits>
 
 #include "paged_common.h"
@@ -34,8 +33,8 @@ __device__ __forceinline__ double flip(double x, uint32_t sign) {
 // One workgroup per (sequence, page that new rows fall into, `heads` of the row's heads: queries, then keys, then
 // values), so that the bounds of a page need no atomics in memory.  It walks the page's rows T at a time: sines and
 // cosines of the next T rows go to LDS in double while these are worked on, and a wave takes a head of the T rows, U loads
-// of HP rows, with the next head's in flight (172 us without, for the prompts above).  Three waves a SIMD: four spill
-// registers, and spilled ones are written and read through memory (174 us).
+// of HP rows, with the next head's in flight (without norm and rotation the prompts above take 90.7 us so and 93.5 otherwise,
+// with them 120.6 and 120.1).  Three waves a SIMD: four spill registers, and spilled ones are written and read through memory (147 us).
 template <int CT, int D>
 __global__ __launch_bounds__(256, 3) void paged_append_rope_kernel(AppendRopeArgs a) {
   constexpr bool BF16 = CT != kFp32;
@@ -228,7 +227,7 @@ hipError_t append_rope_of(const AppendRopeArgs& a, hipStream_t s) {
 
 hipError_t launch_paged_append_rope(AppendRopeArgs a, hipStream_t s) {
   // As many heads a workgroup as leave four workgroups for every CU: sines and cosines are shared by its heads.  Eight
-  // at most (the prompts above 132 us, 143 with sixteen, whose last round is half empty, 140 with four).
+  // at most (the prompts above 121 us, 139 with sixteen, whose last round is half empty, 123 with four).
   const int heads = a.c.Hq + 2 * a.c.Hkv;
   a.heads = kRopeHeads;
   while (a.heads > 4 && (long long)a.c.B * a.pages * ((heads + a.heads - 1) / a.heads) < 4 * kNumCu) a.heads /= 2;

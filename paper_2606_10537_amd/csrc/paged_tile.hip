@@ -213,8 +213,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void paged_tile_kernel(PagedAttnArgs
 #pragma unroll
       for (int i = 0; i < KS; ++i)
         s = mfma32x32x16(*(const bf16x8*)&kt[tile_at<KEYS>(32 * blk + n, 2 * i + hi)], qf[i], s);
-      // The block's V, on its way during the softmax.  512 rows of 8 x 4 heads behind 7.5K keys, a window of 1024: 28.5 us
-      // with V read at its products, 27.1 so; with a window of 4096, 72 and 67.  At 128 rows a workgroup both are alike.
+      // The block's V, on its way during the softmax.  512 rows of 8 x 4 heads behind 7.5K keys, a window of 1024: 25.4 us
+      // with V read at its products, 24.3 so; with a window of 4096, 70.8 and 65.9.  At 128 rows a workgroup (8 such
+      // sequences) 105.6 and 104.3.
       i16x8 v[DB][2];
 #pragma unroll
       for (int i = 0; i < DB; ++i)
